@@ -380,14 +380,20 @@ def _own(st, c):
                                  clip_low=CLIP_LOW, clip_high=CLIP_HIGH, kl_coef=KL, entropy_coef=ENTROPY,
                                  scale=st["scale"],
                                  grad_dtype=torch.bfloat16 if c["grad"] == "bf16" else torch.float32)
+    # (a training program makes this object once and keeps it)
+    if "tensors" not in st:
+        if c["kind"] == "norm":
+            st["tensors"] = lb.TrainTensors(None, st["grads"])
+        else:
+            m, v, scales = st["state"]
+            st["tensors"] = lb.TrainTensors(st["params"], st["grads"], bits=c["bits"], m=m, v=v, scales=scales)
     if c["kind"] == "norm":
-        return lb.lr_grad_norm(st["grads"])
-    state = lb.AdamState(st["params"], bits=c["bits"], m=st["state"][0], v=st["state"][1], scales=st["state"][2])
-    lb.lr_adamw_update(st["params"], st["grads"], state, st["step"], lr=LR, beta1=BETA1, beta2=BETA2, eps=EPS,
-                       weight_decay=DECAY, norm=st["norm"], max_norm=MAX_NORM, seed=st["seed"])
+        return lb.lr_grad_norm(st["tensors"])
+    lb.lr_adamw_update(st["tensors"], st["step"], lr=LR, beta1=BETA1, beta2=BETA2, eps=EPS, weight_decay=DECAY,
+                       norm=st["norm"], max_norm=MAX_NORM, seed=st["seed"])
     if c["bits"] == 32:
         return st["p"], st["m"], st["v"]
-    lb.lr_adamw_moments(state, out_m=st["outs"][0], out_v=st["outs"][1])
+    lb.lr_adamw_moments(st["tensors"], out_m=st["outs"][0], out_v=st["outs"][1])
     return st["p"], st["m_out"], st["v_out"]
 
 
