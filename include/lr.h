@@ -341,6 +341,166 @@ int lr_codesign_backward(const float* d_logits, const float* d_noise, const floa
 int lr_adam_update(float* d_phi, const float* d_grad, float* d_m, float* d_v, int64_t count, int32_t step,
                    float lr, float beta1, float beta2, float eps, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Training device levels by reward.
+ *
+ * lr_codesign_* need dL/dphi, a gradient through the emulated optics.  Where
+ * only a reward is measured (masks loaded on the hardware, its detector read),
+ * the same scores are a policy: pixel r draws level j with probability
+ * softmax(logits_r)_j.  One step draws the masks of a few rollouts
+ * (lr_policy_draw), tries them, forms the gradient of a clipped policy loss
+ * (lr_policy_loss), its norm over all tensors (lr_grad_norm) and moves the
+ * scores (lr_adamw_update).
+ *
+ *   logits  float32 [count][levels], 1 <= levels <= LR_MAX_CHOICES; -inf bars
+ *           a level (a row that makes a choice needs one finite score)
+ *   actions int32 [samples][count], the level each rollout drew for each
+ *           pixel; a negative one stands for no choice (a pixel outside the
+ *           aperture, a rollout that failed): whatever the other arrays hold
+ *           at its place is not looked at, infinities and NaN included
+ * 0 <= samples <= LR_MAX_ROLLOUTS.  samples = 0 or count = 0 enqueues nothing.
+ * Sums over levels, rollouts and pixels run in a fixed order. */
+#define LR_MAX_CHOICES 65536
+#define LR_MAX_ROLLOUTS 1024
+
+/* Type of gradients that are kept between two calls. */
+enum lr_grad_type {
+  LR_GRAD_F32 = 0,
+  LR_GRAD_BF16 = 1   /* rounded to nearest even once, from float32 */
+};
+
+/* Draws levels: d_actions[s][r] = the level j with the largest float32
+ * logits[r][j] + noise[s][r][j], the first on ties and scores that are NaN
+ * left out (0 where all are): a sample of softmax(logits[r]) when the noise is
+ * Gumbel(0, 1).
+ *   d_noise    float32 [samples][count][levels], supplied by the caller
+ *   d_levels   nullable, float32 [levels], the device's phase responses
+ *   d_actions  int32 [samples][count]
+ *   d_logp     nullable, float32 [samples][count]: log softmax(logits[r]) at
+ *              the level drawn
+ *   d_phi      nullable (needs d_levels), float32 [samples][count]: the phase
+ *              of the level drawn; sample s is the mask set of a forward pass
+ * Errors: LR_E_SIZE (levels, samples, count), LR_E_NULL, LR_E_ALIAS, LR_E_HIP. */
+int lr_policy_draw(const float* d_logits, const float* d_noise, const float* d_levels, int32_t samples,
+                   int64_t count, int32_t levels, int32_t* d_actions, float* d_logp, float* d_phi, void* stream);
+
+/* d_logp[s][r] = log softmax(logits[r])[actions[s][r]], as of a reference
+ * policy: 0 where no choice was made, NaN for an action >= levels.
+ * Errors as lr_policy_draw. */
+int lr_policy_logp(const float* d_logits, const int32_t* d_actions, int32_t samples, int64_t count,
+                   int32_t levels, float* d_logp, void* stream);
+
+/* The clipped policy loss and its gradient.  With logp of the choice under
+ * the present logits, ratio = exp(logp - old_logp), d = ref_logp - logp,
+ * advantage A and the row's entropy H = -sum_j p_j log p_j, a choice costs
+ *   l = -min(ratio A, clip(ratio, 1 - clip_low, 1 + clip_high) A)
+ *       + kl_coef (exp(d) - d - 1) - entropy_coef H
+ * and the loss is scale times the sum over all choices made (scale =
+ * 1 / (choices made) for a mean; a batch worked in parts keeps the whole's).
+ *   dL/dlogits[r][j] = sum over the row's choices of
+ *       scale ((j = action) - p_j) dl/dlogp + scale entropy_coef p_j (log p_j + H)
+ * where dl/dlogp = -ratio A (0 where the clipped term is the smaller) +
+ * kl_coef (1 - exp(d)).  Which side of a clip border a ratio lies on is
+ * decided to about 1e-9.
+ *   d_old_logp    float32 [samples][count], when the levels were drawn
+ *   d_ref_logp    nullable (no KL term), float32 [samples][count]
+ *   d_advantages  float32 [samples], or with per_choice != 0 [samples][count]
+ *   d_loss        nullable float32 scalar
+ *   d_terms       nullable float32 [4]: scale times the sums of -min(...),
+ *                 exp(d) - d - 1, H, and the number of choices on the clipped
+ *                 side
+ *   d_grad_logits nullable [count][levels] of grad_type, overwritten; zero in
+ *                 rows without a choice
+ * At least one output.  An action >= levels makes the loss, the terms and the
+ * row's gradient NaN.
+ *   d_work        lr_policy_workspace_size() bytes, aligned to 8
+ * Errors: LR_E_ARG (grad_type; a coefficient not finite; clip_low outside
+ * [0, 1], clip_high < 0), LR_E_SIZE, LR_E_NULL, LR_E_WORKSPACE, LR_E_ALIAS,
+ * LR_E_HIP. */
+typedef struct lr_policy {
+  float clip_low;
+  float clip_high;
+  float kl_coef;
+  float entropy_coef;
+  float scale;
+} lr_policy;
+int64_t lr_policy_workspace_size(void);
+int lr_policy_loss(const lr_policy* policy, const float* d_logits, const int32_t* d_actions,
+                   const float* d_old_logp, const float* d_ref_logp, const float* d_advantages,
+                   int32_t per_choice, int32_t samples, int64_t count, int32_t levels, float* d_loss,
+                   float* d_terms, int32_t grad_type, void* d_grad_logits, void* d_work, size_t work_bytes,
+                   void* stream);
+
+/* One tensor of an optimiser step; the struct is host memory, read during the
+ * call.  Tensors of the list may start anywhere their type allows. */
+typedef struct lr_param {
+  float* d_param;      /* float32 [count] */
+  const void* d_grad;  /* [count] of the call's grad_type */
+  void* d_m;           /* moments: float32 [count], or one byte a value */
+  void* d_v;
+  float* d_scales;     /* 8-bit moments: float32 [ceil(count / LR_STATE_BLOCK)][2] */
+  int64_t count;       /* >= 0 */
+} lr_param;
+
+/* 2-norm over the gradients of all tensors (only d_grad and count are read):
+ * d_norm[0] = sqrt(sum g^2), summed in float64 in a fixed order (a captured
+ * call and an eager one agree); 0 for no values.
+ *   d_work  lr_grad_norm_workspace_size(num) bytes, aligned to 8
+ * Errors: LR_E_ARG (grad_type), LR_E_SIZE (num < 0 or > LR_MAX_PARAMS, a
+ * count < 0), LR_E_NULL, LR_E_WORKSPACE, LR_E_ALIAS, LR_E_HIP. */
+#define LR_MAX_PARAMS 65536
+int64_t lr_grad_norm_workspace_size(int32_t num);
+int lr_grad_norm(const lr_param* params, int32_t num, int32_t grad_type, float* d_norm, void* d_work,
+                 size_t work_bytes, void* stream);
+
+/* One AdamW step over all tensors of the list, in place:
+ *   g' = c g,  c = max_norm / norm where norm > max_norm, else 1
+ *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2
+ *   p = p (1 - lr weight_decay)
+ *       - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * with norm = d_norm[0] as lr_grad_norm leaves it, read when the step runs; a
+ * norm that is not finite leaves every tensor as it was, and a NULL d_norm
+ * clips nothing.  step counts from 1; a captured call repeats its step and
+ * seed.  state_type:
+ *   LR_STATE_F32   d_m, d_v float32, zero before step 1
+ *   LR_STATE_8BIT  d_m, d_v one byte a value and d_scales, all zero before
+ *     step 1.  The LR_STATE_BLOCK values from a multiple of LR_STATE_BLOCK on
+ *     share two scales, u = 2^(E - 127) with E the largest biased float32
+ *     exponent among the block's moments (at least 27).  With f = code & 7:
+ *       m: the high bit is the sign, c the other seven, e = c >> 3:
+ *          2 u (1 + f/8) 2^(e - 15), or for e = 0  2 u (f/8) 2^-14
+ *       v: all eight bits are c:
+ *          2 u (1 + f/8) 2^(e - 31), or for e = 0  2 u (f/8) 2^-30
+ *     A step forms m and v in float32, every product and sum rounded as it
+ *     stands above with (1 - beta) g'^2 as (1 - beta) (g' g'), moves the
+ *     parameters by them and then stores them rounded at random, up with the
+ *     probability of the distance: a step of 1 - beta2 is less than the
+ *     distance of two codes, and rounding to nearest would hold v for ever.
+ *     A v above zero does not become zero.  The random bits are a function of
+ *     seed, the tensor's place in the list and the value's index: give each
+ *     step another seed.  A block in which a moment reaches 2^126 or is not
+ *     finite turns to NaN.
+ * No two buffers of the call may overlap (gradients may be read twice).
+ * Errors: LR_E_SIZE (num < 0 or > LR_MAX_PARAMS, a count < 0, step < 1),
+ * LR_E_ARG (types; lr, eps or weight_decay not finite, eps or weight_decay
+ * < 0, a beta not in [0, 1), max_norm not > 0), LR_E_NULL, LR_E_ALIAS, LR_E_HIP. */
+#define LR_STATE_BLOCK 256
+enum lr_state_type {
+  LR_STATE_F32 = 0,
+  LR_STATE_8BIT = 1
+};
+int lr_adamw_update(const lr_param* params, int32_t num, int32_t grad_type, int32_t state_type, int32_t step,
+                    float lr, float beta1, float beta2, float eps, float weight_decay, const float* d_norm,
+                    float max_norm, uint32_t seed, void* stream);
+
+/* The values that 8-bit moments stand for (inspection, checkpoints): for every
+ * tensor i of the list, d_m_out[i] and d_v_out[i] (host arrays of device
+ * pointers) receive float32 [count] from its d_m, d_v and d_scales.
+ * Errors: LR_E_SIZE, LR_E_NULL, LR_E_ALIAS (an output overlaps any other
+ * buffer), LR_E_HIP. */
+int lr_adamw_moments(const lr_param* params, int32_t num, float* const* d_m_out, float* const* d_v_out,
+                     void* stream);
+
 /* Human-readable name of an lr_status. */
 const char* lr_status_string(int status);
 

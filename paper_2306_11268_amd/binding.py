@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 from typing import Optional, Sequence
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "liblr.so")
@@ -28,6 +28,14 @@ LR_OP_FORWARD = 1
 LR_OP_BACKWARD = 2
 LR_LOSS_SOFTMAX_CE = 0
 LR_LOSS_SOFTMAX_MSE = 1
+LR_MAX_CHOICES = 65536
+LR_MAX_ROLLOUTS = 1024
+LR_MAX_PARAMS = 65536
+LR_GRAD_F32 = 0
+LR_GRAD_BF16 = 1
+LR_STATE_BLOCK = 256
+LR_STATE_F32 = 0
+LR_STATE_8BIT = 1
 
 EXPORTS = (
     "lr_tf_build", "lr_workspace_size", "lr_saved_size",
@@ -35,6 +43,8 @@ EXPORTS = (
     "lr_detector_readout", "lr_donn_forward", "lr_donn_backward",
     "lr_loss", "lr_adam_update", "lr_codesign_phase", "lr_codesign_backward",
     "lr_layer_norm_workspace_size", "lr_layer_norm", "lr_layer_norm_backward",
+    "lr_policy_draw", "lr_policy_logp", "lr_policy_workspace_size", "lr_policy_loss",
+    "lr_grad_norm_workspace_size", "lr_grad_norm", "lr_adamw_update", "lr_adamw_moments",
     "lr_status_string", "lr_kernel_timing", "lr_kernel_timing_report", "lr_version",
 )
 
@@ -50,6 +60,16 @@ class LrDonn(ctypes.Structure):
         ("gamma", c_float), ("det", LrDetector), ("d_H", c_void_p), ("flags", c_int32),
         ("d_skip", c_void_p),
     ]
+
+
+class LrPolicy(ctypes.Structure):
+    _fields_ = [("clip_low", c_float), ("clip_high", c_float), ("kl_coef", c_float), ("entropy_coef", c_float),
+                ("scale", c_float)]
+
+
+class LrParam(ctypes.Structure):
+    _fields_ = [("d_param", c_void_p), ("d_grad", c_void_p), ("d_m", c_void_p), ("d_v", c_void_p),
+                ("d_scales", c_void_p), ("count", c_int64)]
 
 
 class LrError(RuntimeError):
@@ -93,6 +113,18 @@ def load() -> ctypes.CDLL:
     lib.lr_layer_norm_workspace_size.restype = c_int64
     lib.lr_layer_norm.argtypes = [P, c_int32, c_int64, c_float, P, P, P, c_size_t, P]
     lib.lr_layer_norm_backward.argtypes = [P, P, P, c_int32, c_int64, P, P, c_size_t, P]
+    lib.lr_policy_draw.argtypes = [P, P, P, c_int32, c_int64, c_int32, P, P, P, P]
+    lib.lr_policy_logp.argtypes = [P, P, c_int32, c_int64, c_int32, P, P]
+    lib.lr_policy_workspace_size.argtypes = []
+    lib.lr_policy_workspace_size.restype = c_int64
+    lib.lr_policy_loss.argtypes = [POINTER(LrPolicy), P, P, P, P, P, c_int32, c_int32, c_int64, c_int32, P, P, c_int32,
+                                   P, P, c_size_t, P]
+    lib.lr_grad_norm_workspace_size.argtypes = [c_int32]
+    lib.lr_grad_norm_workspace_size.restype = c_int64
+    lib.lr_grad_norm.argtypes = [P, c_int32, c_int32, P, P, c_size_t, P]
+    lib.lr_adamw_update.argtypes = [P, c_int32, c_int32, c_int32, c_int32, c_float, c_float, c_float, c_float, c_float,
+                                    P, c_float, c_uint32, P]
+    lib.lr_adamw_moments.argtypes = [P, c_int32, P, P, P]
     lib.lr_status_string.argtypes = [ctypes.c_int]
     lib.lr_status_string.restype = c_char_p
     lib.lr_kernel_timing.argtypes = [c_int32]
@@ -496,3 +528,245 @@ def multichannel_train_step(nets, amps, phis, saveds, labels, kind: int = LR_LOS
     grads = [lr_donn_backward(net, phi, saved, grad_sums=grad_sums)[0]
              for net, phi, saved in zip(nets, phis, saveds)]
     return loss, merged, grads
+
+
+# ---------------------------------------------------------------------------
+# Training device levels by reward
+# ---------------------------------------------------------------------------
+
+def _run_on(device, fn, *args) -> int:
+    """fn(*args, stream) with the device current and on its current stream."""
+    torch = _torch()
+    if torch.cuda.current_device() == device.index:
+        return fn(*args, _stream(device))
+    with torch.cuda.device(device):
+        return fn(*args, _stream(device))
+
+
+def _at(device, t, dtype, shape, name) -> Optional[int]:
+    """Address of a contiguous tensor of this type and shape on the device, or None."""
+    if t is None:
+        return None
+    if t.device != device or t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _policy_shapes(logits, samples: int):
+    """(pixels, levels, shape of one array of choices) of logits [..., K]."""
+    if not logits.is_cuda or logits.dim() < 1:
+        raise ValueError("logits must be a device tensor [..., levels]")
+    k = int(logits.shape[-1])
+    rows = logits.shape[:-1]
+    return rows.numel(), k, (samples, *rows)
+
+
+def lr_policy_draw(logits, noise, levels=None, want_logp: bool = True, out_actions=None, out_logp=None, out_phi=None):
+    """Levels drawn for the rollouts of one step: scores [..., K], Gumbel draws
+    [S, ..., K] and the device's phase levels [K] give (actions int32 [S, ...],
+    their log-probabilities [S, ...], the phase masks [S, ...]); without
+    levels the last is None, without want_logp the second."""
+    torch = _torch()
+    dev = logits.device
+    s = int(noise.shape[0])
+    count, k, shape = _policy_shapes(logits, s)
+    if out_actions is None:
+        out_actions = torch.empty(shape, dtype=torch.int32, device=dev)
+    if out_logp is None and want_logp:
+        out_logp = torch.empty(shape, dtype=torch.float32, device=dev)
+    if out_phi is None and levels is not None:
+        out_phi = torch.empty(shape, dtype=torch.float32, device=dev)
+    _check(_run_on(dev, load().lr_policy_draw,
+                   _at(dev, logits, torch.float32, logits.shape, "logits"),
+                   _at(dev, noise, torch.float32, (*shape, k), "noise"),
+                   _at(dev, levels, torch.float32, (k,), "levels"), s, count, k,
+                   _at(dev, out_actions, torch.int32, shape, "actions"),
+                   _at(dev, out_logp, torch.float32, shape, "logp"),
+                   _at(dev, out_phi, torch.float32, shape, "phi")), "lr_policy_draw")
+    return out_actions, out_logp, out_phi
+
+
+def lr_policy_logp(logits, actions, out=None):
+    """Log-probabilities [S, ...] of levels already drawn, as under a reference
+    policy's scores [..., K]; 0 where an action is negative."""
+    torch = _torch()
+    dev = logits.device
+    s = int(actions.shape[0])
+    count, k, shape = _policy_shapes(logits, s)
+    if out is None:
+        out = torch.empty(shape, dtype=torch.float32, device=dev)
+    _check(_run_on(dev, load().lr_policy_logp, _at(dev, logits, torch.float32, logits.shape, "logits"),
+                   _at(dev, actions, torch.int32, shape, "actions"), s, count, k,
+                   _at(dev, out, torch.float32, shape, "logp")), "lr_policy_logp")
+    return out
+
+
+def lr_policy_loss(logits, actions, old_logp, advantages, ref_logp=None, clip_low: float = 0.2, clip_high: float = 0.2,
+                   kl_coef: float = 0.0, entropy_coef: float = 0.0, scale: Optional[float] = None, grad_dtype=None,
+                   want_loss: bool = True, want_grad: bool = True, out_grad=None):
+    """Clipped policy loss of the levels drawn: (loss, terms [4], dL/dlogits
+    [..., K] in grad_dtype, float32 or bfloat16).
+
+    logits [..., K]; actions, old_logp and ref_logp [S, ...] (a negative
+    action: no choice there); advantages [S], or [S, ...] for every choice.
+    scale defaults to 1 / (S * pixels): give 1 / (choices made) for the mean
+    where some are missing.  terms: scale times the sums of the clipped term,
+    of the KL estimate and of the entropy, and the clipped share."""
+    torch = _torch()
+    dev = logits.device
+    s = int(actions.shape[0])
+    count, k, shape = _policy_shapes(logits, s)
+    per_choice = tuple(advantages.shape) == shape and advantages.dim() > 1
+    grad_dtype = torch.float32 if grad_dtype is None else grad_dtype
+    if grad_dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"grad_dtype must be float32 or bfloat16, got {grad_dtype}")
+    if want_grad and out_grad is None:
+        out_grad = torch.empty(logits.shape, dtype=grad_dtype, device=dev)
+    both = torch.empty(5, dtype=torch.float32, device=dev) if want_loss else None
+    work = torch.empty(int(load().lr_policy_workspace_size()), dtype=torch.uint8, device=dev)
+    policy = LrPolicy(clip_low, clip_high, kl_coef, entropy_coef, 1.0 / max(1, s * count) if scale is None else scale)
+    at = both.data_ptr() if want_loss else None
+    _check(_run_on(dev, load().lr_policy_loss, ctypes.byref(policy),
+                   _at(dev, logits, torch.float32, logits.shape, "logits"),
+                   _at(dev, actions, torch.int32, shape, "actions"),
+                   _at(dev, old_logp, torch.float32, shape, "old_logp"),
+                   _at(dev, ref_logp, torch.float32, shape, "ref_logp"),
+                   _at(dev, advantages, torch.float32, shape if per_choice else (s,), "advantages"),
+                   1 if per_choice else 0, s, count, k, at, at + 4 if want_loss else None,
+                   LR_GRAD_BF16 if grad_dtype == torch.bfloat16 else LR_GRAD_F32,
+                   _at(dev, out_grad, grad_dtype, logits.shape, "grad_logits"), work.data_ptr(), work.numel()),
+           "lr_policy_loss")
+    return (both[0], both[1:], out_grad) if want_loss else (None, None, out_grad)
+
+
+class TrainTensors:
+    """The tensors of an optimiser step: parameters, gradients and AdamW moments.
+
+    params: float32 tensors (None for lr_grad_norm alone); grads: one for each,
+    all float32 or all bfloat16.  bits: 32 or 8, of the moments, which are
+    allocated as zeros unless m, v (and for 8 bits scales) are given.  The
+    object keeps the tensors' memory; their values may change between steps,
+    and set_grads puts other gradients in place."""
+
+    def __init__(self, params, grads, bits: int = 32, m=None, v=None, scales=None):
+        torch = _torch()
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        self.bits = bits
+        self.num = len(grads)
+        self._table = (LrParam * max(self.num, 1))()
+        self._held = {}
+        like = grads if params is None else params
+        self.device = like[0].device if self.num else torch.device("cuda", torch.cuda.current_device())
+        self._counts = [int(t.numel()) for t in like]
+        for i, n in enumerate(self._counts):
+            self._table[i].count = n
+        if params is not None:
+            mtype = torch.uint8 if bits == 8 else torch.float32
+            new = lambda: [torch.zeros(n, dtype=mtype, device=self.device) for n in self._counts]  # noqa: E731
+            self._hold("d_param", params, torch.float32, self._counts)
+            self.params = list(params)
+            self.m = self._hold("d_m", new() if m is None else m, mtype, self._counts)
+            self.v = self._hold("d_v", new() if v is None else v, mtype, self._counts)
+            if bits == 8:
+                blocks = [-(-n // LR_STATE_BLOCK) for n in self._counts]
+                if scales is None:
+                    scales = [torch.zeros((b, 2), dtype=torch.float32, device=self.device) for b in blocks]
+                self.scales = self._hold("d_scales", scales, torch.float32, [2 * b for b in blocks])
+        self.set_grads(grads)
+
+    def _hold(self, field, tensors, dtype, counts):
+        """Checks one kind of tensors and puts their addresses into the table."""
+        tensors = list(tensors)
+        if len(tensors) != len(counts):
+            raise ValueError(f"{field}: {len(tensors)} tensors for {len(counts)}")
+        for t, n in zip(tensors, counts):
+            if t.device != self.device or not t.is_cuda or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+                raise ValueError(f"{field}: a contiguous {dtype} tensor of {n} values on {self.device} is needed, "
+                                 f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        # (a second tensor on the same memory keeps it, whatever becomes of the caller's)
+        held = [t.detach() for t in tensors]
+        self._held[field] = held
+        for i, t in enumerate(held):
+            setattr(self._table[i], field, t.data_ptr())
+        return tensors
+
+    def set_grads(self, grads) -> None:
+        torch = _torch()
+        dtype = grads[0].dtype if len(grads) else torch.float32
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"gradients must be float32 or bfloat16, got {dtype}")
+        self._hold("d_grad", grads, dtype, self._counts)
+        self.grad_type = LR_GRAD_BF16 if dtype == torch.bfloat16 else LR_GRAD_F32
+
+
+def lr_grad_norm(grads, out=None):
+    """2-norm over all gradients (a TrainTensors, or a list of tensors of one
+    type), a float32 scalar on the device."""
+    torch = _torch()
+    t = grads if isinstance(grads, TrainTensors) else TrainTensors(None, grads)
+    if out is None:
+        out = torch.empty((), dtype=torch.float32, device=t.device)
+    work = torch.empty(int(load().lr_grad_norm_workspace_size(t.num)), dtype=torch.uint8, device=t.device)
+    _check(_run_on(t.device, load().lr_grad_norm, t._table, t.num, t.grad_type,
+                   _at(t.device, out, torch.float32, (), "norm"), work.data_ptr(), work.numel()), "lr_grad_norm")
+    return out
+
+
+def lr_adamw_update(tensors: TrainTensors, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+                    eps: float = 1e-8, weight_decay: float = 0.0, norm=None, max_norm: float = float("inf"),
+                    seed: Optional[int] = None) -> None:
+    """One AdamW step over all tensors, in place.  norm: lr_grad_norm's scalar;
+    the gradients are then scaled down to max_norm, and a norm that is not
+    finite leaves everything as it was.  seed (of the rounding of 8-bit
+    moments, a 32-bit number) defaults to the step."""
+    torch = _torch()
+    if "d_param" not in tensors._held:
+        raise ValueError("these tensors have no parameters")
+    _check(_run_on(tensors.device, load().lr_adamw_update, tensors._table, tensors.num, tensors.grad_type,
+                   LR_STATE_8BIT if tensors.bits == 8 else LR_STATE_F32, int(step), lr, beta1, beta2, eps,
+                   weight_decay, _at(tensors.device, norm, torch.float32, (), "norm"), max_norm,
+                   (int(step) if seed is None else int(seed)) & 0xFFFFFFFF), "lr_adamw_update")
+
+
+def lr_adamw_moments(tensors: TrainTensors, out_m=None, out_v=None):
+    """The moments as float32, ([m of each tensor], [v of each]): what the codes
+    of 8-bit moments stand for, or the tensors themselves where they are float32."""
+    torch = _torch()
+    if "d_param" not in tensors._held:
+        raise ValueError("these tensors have no parameters")
+    if tensors.bits == 32:
+        if out_m is not None or out_v is not None:
+            raise ValueError("moments of 32 bits are float32 tensors already")
+        return tensors.m, tensors.v
+    outs = []
+    for given in (out_m, out_v):
+        if given is None:
+            given = [torch.empty(n, dtype=torch.float32, device=tensors.device) for n in tensors._counts]
+        if len(given) != tensors.num:
+            raise ValueError(f"{len(given)} outputs for {tensors.num} tensors")
+        outs.append(list(given))
+    at = [(c_void_p * max(tensors.num, 1))(*[_at(tensors.device, t, torch.float32, (n,), "moments")
+                                             for t, n in zip(o, tensors._counts)]) for o in outs]
+    _check(_run_on(tensors.device, load().lr_adamw_moments, tensors._table, tensors.num, at[0], at[1]),
+           "lr_adamw_moments")
+    return outs[0], outs[1]
+
+
+def policy_train_step(tensors: TrainTensors, actions, old_logp, advantages, step: int, lr: float,
+                      max_norm: float = 1.0, weight_decay: float = 0.0, **policy):
+    """One step on the codesign scores from the rewards of a few rollouts,
+    through the C ABI.
+
+    The scores [..., K] are the first parameter of tensors.  The policy loss
+    (policy: the arguments of lr_policy_loss) writes their gradient into
+    tensors' first gradient, the norm is taken over all gradients, and the
+    clipped AdamW step moves every parameter.  Returns (loss, terms, norm)."""
+    logits = tensors.params[0]
+    grad = tensors._held["d_grad"][0].view(logits.shape)
+    loss, terms, _ = lr_policy_loss(logits, actions, old_logp, advantages, grad_dtype=grad.dtype, out_grad=grad,
+                                    **policy)
+    norm = lr_grad_norm(tensors)
+    lr_adamw_update(tensors, step, lr, weight_decay=weight_decay, norm=norm, max_norm=max_norm)
+    return loss, terms, norm

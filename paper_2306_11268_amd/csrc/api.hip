@@ -120,6 +120,8 @@ bool outputs_alias(std::initializer_list<Span> outputs, std::initializer_list<Sp
   return false;
 }
 
+constexpr int64_t kMaxValues = int64_t(1) << 56;  // values of a buffer: its bytes fit 63 bits
+
 int validate_detector(const lr_detector& d, int n) {
   if (d.num < 0 || d.num > LR_MAX_REGIONS) return LR_E_ARG;
   if (d.num == 0) return LR_OK;
@@ -554,6 +556,85 @@ void fraunhofer_table(double lam, double pitch, double z, int M, std::vector<cd>
       const double sgn = ((x + y) & 1) ? -1.0 : 1.0;
       Q[static_cast<size_t>(y) * M + x] = sgn * pre * std::polar(1.0, k * (xo * xo + yo * yo) / (2.0 * z));
     }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Training device levels by reward: checks of the policy and optimiser calls
+// ---------------------------------------------------------------------------
+int policy_check(int32_t samples, int64_t count, int32_t levels) {
+  if (levels < 1 || levels > LR_MAX_CHOICES || samples < 0 || samples > LR_MAX_ROLLOUTS || count < 0)
+    return LR_E_SIZE;
+  // (the bytes of the largest array, [samples][count][levels], stay below 2^63)
+  if (count > kMaxValues / levels / std::max<int64_t>(samples, 1)) return LR_E_SIZE;
+  return LR_OK;
+}
+
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+struct Range {
+  const char* at;
+  size_t bytes;
+  bool out;
+};
+
+// An output range overlaps any other (inputs may share memory).  Sorts the ranges.
+bool ranges_alias(std::vector<Range>& v) {
+  std::sort(v.begin(), v.end(), [](const Range& a, const Range& b) { return a.at < b.at; });
+  const char* end = nullptr;      // of all ranges so far
+  const char* out_end = nullptr;  // of the output ranges so far
+  for (const Range& r : v) {
+    if (r.bytes == 0) continue;
+    if (r.at < out_end || (r.out && r.at < end)) return true;
+    end = std::max(end, r.at + r.bytes);
+    if (r.out) out_end = std::max(out_end, r.at + r.bytes);
+  }
+  return false;
+}
+
+int params_check(const lr_param* params, int32_t num) {
+  if (num < 0 || num > LR_MAX_PARAMS) return LR_E_SIZE;
+  if (num > 0 && !params) return LR_E_NULL;
+  int64_t all = 0;
+  for (int32_t i = 0; i < num; ++i) {
+    if (params[i].count < 0 || params[i].count > kMaxValues - all) return LR_E_SIZE;
+    all += params[i].count;
+  }
+  return LR_OK;
+}
+
+// The tensors in lists of one launch each, empty ones left out; the random
+// bits' keys count every tensor.
+std::vector<lr::TensorList> tensor_lists(const lr_param* params, int32_t num, uint32_t seed) {
+  std::vector<lr::TensorList> lists;
+  for (int32_t i = 0; i < num; ++i) {
+    const lr_param& p = params[i];
+    if (p.count == 0) continue;
+    if (lists.empty() || lists.back().num == lr::kTensorsPerLaunch) lists.push_back(lr::TensorList{});
+    lr::TensorList& l = lists.back();
+    lr::TensorEntry& t = l.t[l.num++];
+    t.param = p.d_param;
+    t.grad = p.d_grad;
+    t.m = p.d_m;
+    t.v = p.d_v;
+    t.scales = p.d_scales;
+    t.count = static_cast<long long>(p.count);
+    t.chunk0 = l.chunks;
+    t.key = lr::tensor_key(seed, static_cast<uint32_t>(i));
+    l.chunks += (t.count + lr::kTensorChunk - 1) / lr::kTensorChunk;
+  }
+  return lists;
+}
+
+size_t scale_bytes(int64_t count) { return static_cast<size_t>((count + LR_STATE_BLOCK - 1) / LR_STATE_BLOCK) * 8; }
+
+// No C++ exception (out of host memory) leaves an entry point.
+template <class F>
+int no_throw(F&& f) {
+  try {
+    return f();
+  } catch (...) {
+    return LR_E_HIP;
   }
 }
 
@@ -1245,6 +1326,195 @@ int lr_adam_update(float* d_phi, const float* d_grad, float* d_m, float* d_v, in
   return run_timed("adam", st, [&] {
     return lr::launch_adam(d_phi, d_grad, d_m, d_v, static_cast<long long>(count), lr, beta1, beta2, eps,
                            static_cast<float>(bc1), static_cast<float>(bc2), st);
+  });
+}
+
+int lr_policy_draw(const float* d_logits, const float* d_noise, const float* d_levels, int32_t samples, int64_t count,
+                   int32_t levels, int32_t* d_actions, float* d_logp, float* d_phi, void* stream) {
+  LR_TRY(policy_check(samples, count, levels));
+  if (count == 0 || samples == 0) return LR_OK;
+  if (!d_logits || !d_noise || !d_actions || (d_phi && !d_levels)) return LR_E_NULL;
+  {
+    const size_t sc = static_cast<size_t>(count) * levels * 4;
+    const size_t ch = static_cast<size_t>(count) * samples * 4;
+    if (outputs_alias({{d_actions, ch}, {d_logp, ch}, {d_phi, ch}},
+                      {{d_logits, sc}, {d_noise, sc * samples}, {d_levels, static_cast<size_t>(levels) * 4}}))
+      return LR_E_ALIAS;
+  }
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const lr::PolicyDrawArgs a{d_logits, d_noise, d_levels, samples, levels, static_cast<long long>(count),
+                             d_actions, d_logp, d_phi};
+  return run_timed("policy_draw", st, [&] { return lr::launch_policy_draw(a, st); });
+}
+
+int lr_policy_logp(const float* d_logits, const int32_t* d_actions, int32_t samples, int64_t count, int32_t levels,
+                   float* d_logp, void* stream) {
+  LR_TRY(policy_check(samples, count, levels));
+  if (count == 0 || samples == 0) return LR_OK;
+  if (!d_logits || !d_actions || !d_logp) return LR_E_NULL;
+  {
+    const size_t ch = static_cast<size_t>(count) * samples * 4;
+    if (outputs_alias({{d_logp, ch}}, {{d_logits, static_cast<size_t>(count) * levels * 4}, {d_actions, ch}}))
+      return LR_E_ALIAS;
+  }
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const lr::PolicyDrawArgs a{d_logits, nullptr, nullptr, samples, levels, static_cast<long long>(count),
+                             const_cast<int32_t*>(d_actions), d_logp, nullptr};
+  return run_timed("policy_logp", st, [&] { return lr::launch_policy_draw(a, st); });
+}
+
+int64_t lr_policy_workspace_size(void) { return static_cast<int64_t>(lr::kPolicyParts) * 4 * sizeof(double); }
+
+int lr_policy_loss(const lr_policy* policy, const float* d_logits, const int32_t* d_actions, const float* d_old_logp,
+                   const float* d_ref_logp, const float* d_advantages, int32_t per_choice, int32_t samples,
+                   int64_t count, int32_t levels, float* d_loss, float* d_terms, int32_t grad_type,
+                   void* d_grad_logits, void* d_work, size_t work_bytes, void* stream) {
+  if (!policy) return LR_E_NULL;
+  if (grad_type != LR_GRAD_F32 && grad_type != LR_GRAD_BF16) return LR_E_ARG;
+  if (!(policy->clip_low >= 0.f && policy->clip_low <= 1.f) || !(policy->clip_high >= 0.f) ||
+      !std::isfinite(policy->clip_high) || !std::isfinite(policy->kl_coef) || !std::isfinite(policy->entropy_coef) ||
+      !std::isfinite(policy->scale))
+    return LR_E_ARG;
+  LR_TRY(policy_check(samples, count, levels));
+  if (!d_loss && !d_terms && !d_grad_logits) return LR_E_NULL;
+  if (count == 0 || samples == 0) return LR_OK;
+  if (!d_logits || !d_actions || !d_old_logp || !d_advantages || !d_work) return LR_E_NULL;
+  if (work_bytes < static_cast<size_t>(lr_policy_workspace_size()) || !aligned(d_work, 8)) return LR_E_WORKSPACE;
+  {
+    const size_t cl = static_cast<size_t>(count) * levels;
+    const size_t ch = static_cast<size_t>(count) * samples * 4;
+    if (outputs_alias({{d_loss, 4}, {d_terms, 16}, {d_grad_logits, cl * (grad_type == LR_GRAD_BF16 ? 2 : 4)},
+                       {d_work, static_cast<size_t>(lr_policy_workspace_size())}},
+                      {{d_logits, cl * 4}, {d_actions, ch}, {d_old_logp, ch}, {d_ref_logp, ch},
+                       {d_advantages, per_choice ? ch : static_cast<size_t>(samples) * 4}}))
+      return LR_E_ALIAS;
+  }
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const lr::PolicyLossArgs a{d_logits, d_actions, d_old_logp, d_ref_logp, d_advantages, per_choice ? 1 : 0, samples,
+                             levels, grad_type == LR_GRAD_BF16 ? 1 : 0, static_cast<long long>(count),
+                             policy->clip_low, policy->clip_high, policy->kl_coef, policy->entropy_coef,
+                             policy->scale, d_grad_logits, d_loss, d_terms, static_cast<double*>(d_work)};
+  return run_timed("policy_loss", st, [&] { return lr::launch_policy_loss(a, st); });
+}
+
+int64_t lr_grad_norm_workspace_size(int32_t num) {
+  if (num < 0 || num > LR_MAX_PARAMS) return -static_cast<int64_t>(LR_E_SIZE);
+  const int64_t lists = std::max<int64_t>(1, (num + lr::kTensorsPerLaunch - 1) / lr::kTensorsPerLaunch);
+  return lists * lr::kNormParts * static_cast<int64_t>(sizeof(double));
+}
+
+int lr_grad_norm(const lr_param* params, int32_t num, int32_t grad_type, float* d_norm, void* d_work,
+                 size_t work_bytes, void* stream) {
+  if (grad_type != LR_GRAD_F32 && grad_type != LR_GRAD_BF16) return LR_E_ARG;
+  LR_TRY(params_check(params, num));
+  if (!d_norm || !d_work) return LR_E_NULL;
+  const size_t need = static_cast<size_t>(lr_grad_norm_workspace_size(num));
+  if (work_bytes < need || !aligned(d_work, 8)) return LR_E_WORKSPACE;
+  const size_t gb = grad_type == LR_GRAD_BF16 ? 2 : 4;
+  if (overlaps(d_norm, 4, d_work, need)) return LR_E_ALIAS;
+  for (int32_t i = 0; i < num; ++i) {
+    if (params[i].count > 0 && !params[i].d_grad) return LR_E_NULL;
+    const size_t bytes = static_cast<size_t>(params[i].count) * gb;
+    if (overlaps(params[i].d_grad, bytes, d_norm, 4) || overlaps(params[i].d_grad, bytes, d_work, need))
+      return LR_E_ALIAS;
+  }
+  return no_throw([&] {
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const std::vector<lr::TensorList> lists = tensor_lists(params, num, 0);
+    return run_timed("grad_norm", st, [&] {
+      return lr::launch_grad_norm(lists.data(), static_cast<int>(lists.size()), grad_type == LR_GRAD_BF16 ? 1 : 0,
+                                  static_cast<double*>(d_work), d_norm, st);
+    });
+  });
+}
+
+int lr_adamw_update(const lr_param* params, int32_t num, int32_t grad_type, int32_t state_type, int32_t step, float lr,
+                    float beta1, float beta2, float eps, float weight_decay, const float* d_norm, float max_norm,
+                    uint32_t seed, void* stream) {
+  if (step < 1) return LR_E_SIZE;
+  if ((grad_type != LR_GRAD_F32 && grad_type != LR_GRAD_BF16) ||
+      (state_type != LR_STATE_F32 && state_type != LR_STATE_8BIT))
+    return LR_E_ARG;
+  if (!std::isfinite(lr) || !(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f) || !(eps >= 0.f) ||
+      !std::isfinite(eps) || !(weight_decay >= 0.f) || !std::isfinite(weight_decay) || !(max_norm > 0.f))
+    return LR_E_ARG;
+  LR_TRY(params_check(params, num));
+  const double bc1 = 1.0 - std::pow(static_cast<double>(beta1), step);
+  const double bc2 = 1.0 - std::pow(static_cast<double>(beta2), step);
+  if (!(bc1 > 0.0) || !(bc2 > 0.0)) return LR_E_ARG;
+  const bool bits8 = state_type == LR_STATE_8BIT;
+  return no_throw([&]() -> int {
+    std::vector<Range> ranges;
+    ranges.reserve(static_cast<size_t>(num) * 5 + 1);
+    for (int32_t i = 0; i < num; ++i) {
+      const lr_param& p = params[i];
+      if (p.count == 0) continue;
+      if (!p.d_param || !p.d_grad || !p.d_m || !p.d_v || (bits8 && !p.d_scales)) return LR_E_NULL;
+      const size_t n = static_cast<size_t>(p.count);
+      ranges.push_back({reinterpret_cast<const char*>(p.d_param), n * 4, true});
+      ranges.push_back({static_cast<const char*>(p.d_grad), n * (grad_type == LR_GRAD_BF16 ? 2 : 4), false});
+      ranges.push_back({static_cast<const char*>(p.d_m), n * (bits8 ? 1 : 4), true});
+      ranges.push_back({static_cast<const char*>(p.d_v), n * (bits8 ? 1 : 4), true});
+      if (bits8) ranges.push_back({reinterpret_cast<const char*>(p.d_scales), scale_bytes(p.count), true});
+    }
+    if (ranges.empty()) return LR_OK;
+    if (d_norm) ranges.push_back({reinterpret_cast<const char*>(d_norm), 4, false});
+    if (ranges_alias(ranges)) return LR_E_ALIAS;
+    lr::AdamwArgs a{};
+    a.norm = d_norm;
+    a.max_norm = max_norm;
+    a.b1 = beta1;
+    a.c1 = static_cast<float>(1.0 - static_cast<double>(beta1));
+    a.b2 = beta2;
+    a.c2 = static_cast<float>(1.0 - static_cast<double>(beta2));
+    a.keep = static_cast<float>(1.0 - static_cast<double>(lr) * static_cast<double>(weight_decay));
+    a.rate = static_cast<float>(static_cast<double>(lr) / bc1);
+    a.root = static_cast<float>(1.0 / std::sqrt(bc2));
+    a.eps = eps;
+    a.bf16 = grad_type == LR_GRAD_BF16 ? 1 : 0;
+    a.bits8 = bits8 ? 1 : 0;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const std::vector<lr::TensorList> lists = tensor_lists(params, num, seed);
+    return run_timed(bits8 ? "adamw8" : "adamw", st, [&] {
+      for (const lr::TensorList& l : lists) {
+        const hipError_t e = lr::launch_adamw(l, a, st);
+        if (e != hipSuccess) return e;
+      }
+      return hipSuccess;
+    });
+  });
+}
+
+int lr_adamw_moments(const lr_param* params, int32_t num, float* const* d_m_out, float* const* d_v_out,
+                     void* stream) {
+  LR_TRY(params_check(params, num));
+  if (num > 0 && (!d_m_out || !d_v_out)) return LR_E_NULL;
+  return no_throw([&]() -> int {
+    std::vector<Range> ranges;
+    std::vector<lr_param> outs(params, params + num);
+    for (int32_t i = 0; i < num; ++i) {
+      const lr_param& p = params[i];
+      if (p.count == 0) continue;
+      if (!p.d_m || !p.d_v || !p.d_scales || !d_m_out[i] || !d_v_out[i]) return LR_E_NULL;
+      const size_t n = static_cast<size_t>(p.count);
+      ranges.push_back({static_cast<const char*>(p.d_m), n, false});
+      ranges.push_back({static_cast<const char*>(p.d_v), n, false});
+      ranges.push_back({reinterpret_cast<const char*>(p.d_scales), scale_bytes(p.count), false});
+      ranges.push_back({reinterpret_cast<const char*>(d_m_out[i]), n * 4, true});
+      ranges.push_back({reinterpret_cast<const char*>(d_v_out[i]), n * 4, true});
+      outs[i].d_param = d_m_out[i];
+      outs[i].d_grad = d_v_out[i];
+    }
+    if (ranges_alias(ranges)) return LR_E_ALIAS;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const std::vector<lr::TensorList> lists = tensor_lists(outs.data(), num, 0);
+    return run_timed("adamw_moments", st, [&] {
+      for (const lr::TensorList& l : lists) {
+        const hipError_t e = lr::launch_moments(l, st);
+        if (e != hipSuccess) return e;
+      }
+      return hipSuccess;
+    });
   });
 }
 

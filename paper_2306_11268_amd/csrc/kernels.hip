@@ -1,7 +1,11 @@
 // Helper kernels and the size dispatch of the pass kernels.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
+#include "adamw_impl.hpp"
 #include "kernels.hpp"
+#include "policy_impl.hpp"
 #include "tile.hpp"
 
 namespace lr {

@@ -239,4 +239,77 @@ hipError_t launch_layer_norm(const float* x, int batch, long long count, float e
 hipError_t launch_layer_norm_backward(const float* g, const float* y, const float2* stats, int batch,
                                       long long count, float* dx, float2* part, float2* stats2, hipStream_t st);
 
+
+// Policy over device levels: logits [count][K], actions [samples][count].
+struct PolicyDrawArgs {
+  const float* logits;
+  const float* noise;   // [samples][count][K]: actions are drawn; NULL: they are given
+  const float* levels;  // nullable, [K]
+  int samples;
+  int K;
+  long long count;
+  int32_t* actions;
+  float* logp;  // nullable
+  float* phi;   // nullable
+};
+hipError_t launch_policy_draw(const PolicyDrawArgs& a, hipStream_t st);
+
+constexpr int kPolicyParts = 2048;  // workgroups of the loss kernel, four partial sums each
+struct PolicyLossArgs {
+  const float* logits;
+  const int32_t* actions;
+  const float* old_logp;
+  const float* ref_logp;  // nullable
+  const float* adv;       // [samples], or [samples][count] (per_choice)
+  int per_choice;
+  int samples;
+  int K;
+  int bf16;  // type of grad
+  long long count;
+  float clip_low, clip_high, kl_coef, entropy_coef, scale;
+  void* grad;      // nullable
+  float* loss;     // nullable
+  float* terms;    // nullable, [4]
+  double* part;    // [kPolicyParts][4]
+};
+hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st);
+
+// The tensors of one launch of an optimiser step, worked in chunks of
+// kTensorChunk values (a kernel argument: a launch may be captured).
+constexpr int kTensorChunk = 2048;
+constexpr int kTensorsPerLaunch = 48;
+struct TensorEntry {
+  float* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* scales;
+  long long count;
+  long long chunk0;  // first chunk
+  uint32_t key;      // of the random bits
+};
+struct TensorList {
+  TensorEntry t[kTensorsPerLaunch];
+  long long chunks;
+  int num;
+};
+constexpr int kNormParts = 2048;  // partial sums of one launch
+hipError_t launch_grad_norm(const TensorList* lists, int num, int bf16, double* part, float* norm, hipStream_t st);
+struct AdamwArgs {
+  const float* norm;  // nullable
+  float max_norm;
+  float b1, c1, b2, c2;  // beta, 1 - beta
+  float keep;            // 1 - lr * weight_decay
+  float rate;            // lr / (1 - beta1^step)
+  float root;            // 1 / sqrt(1 - beta2^step)
+  float eps;
+  int bf16;
+  int bits8;
+};
+hipError_t launch_adamw(const TensorList& l, const AdamwArgs& a, hipStream_t st);
+// m and v of 8-bit moments as float32 (into param and grad of the entries).
+hipError_t launch_moments(const TensorList& l, hipStream_t st);
+// First key of the random bits of tensor i.
+uint32_t tensor_key(uint32_t seed, uint32_t i);
+
 }  // namespace lr

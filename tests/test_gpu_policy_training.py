@@ -1,0 +1,166 @@
+"""Device levels trained by reward, as one run: levels drawn, the masks tried in the emulator, the policy loss, the
+norm of its gradient and the optimiser step; eager, on another stream, and recorded as a graph.
+
+Tolerances: what the parts' own tests derive; a step through AdamW turns a gradient's relative error into as much of
+the step, so that scores agree to 1e-4 of the largest step where no gradient is near zero.
+"""
+
+import numpy as np
+import pytest
+
+import oracle.donn as od
+import oracle.training as ot
+from paper_2306_11268_amd import workloads as wl
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lrb():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2306_11268_amd import binding
+    binding.load()
+    return binding
+
+
+def dev(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def host(t):
+    return t.detach().float().cpu().numpy() if t.dtype == torch.bfloat16 else t.detach().cpu().numpy()
+
+
+def gumbel(seed, shape):
+    return np.random.default_rng([230611268, 43, seed]).gumbel(size=shape).astype(np.float32)
+
+
+@pytest.mark.parametrize("bits", (32, 8))
+def test_a_step_from_rollouts_in_the_emulator(lrb, bits):
+    w = wl.scaled(wl.WORKLOADS[3], n=64, layers=2)
+    b, k, s = 4, 16, 5
+    det = wl.ten_class_layout(64)
+    levels = wl.device_levels(w.wid, k)
+    shape = (w.layers, w.n, w.n)
+    scores = wl.codesign_scores(w.wid, shape, k)
+    amp, labels = wl.amplitudes(w, b), wl.labels(w, b)
+    net = lrb.Network(w.wavelength, w.pixel_pitch, w.distance, w.approx, w.n, w.n_fft, w.layers, 1.0,
+                      lrb.Detector(det.size, det.y0, det.x0))
+    x = dev(scores)
+    t = lrb.TrainTensors([x], [torch.zeros_like(x)], bits=bits)
+    noise = gumbel(1, (s, *shape, k))
+    actions, logp, phi = lrb.lr_policy_draw(x, dev(noise), dev(levels))
+
+    # the rollouts' rewards: minus the loss of each mask set
+    rewards = []
+    for i in range(s):
+        sums = lrb.lr_donn_forward(net, dev(amp), phi[i], sums=True)["sums"]
+        rewards.append(-float(lrb.lr_loss(sums, dev(labels))[0]))
+    h = od.transfer_function(w.wavelength, w.pixel_pitch, w.distance, w.approx, w.n_fft)
+    odet = od.Detector(det.size, tuple(det.y0), tuple(det.x0))
+    want_a = ot.policy_draw(scores, noise)
+    assert np.array_equal(host(actions), want_a)
+    want = [-od.softmax_cross_entropy(od.donn_forward(amp, levels[want_a[i]], h, 1.0, odet)["sums"], labels)[0]
+            for i in range(s)]
+    assert np.allclose(rewards, want, rtol=1e-4)
+
+    adv = ((np.array(rewards) - np.mean(rewards)) / (np.std(rewards) + 1e-6)).astype(np.float32)
+    kw = dict(kl_coef=0.02, entropy_coef=0.01, clip_high=0.28)
+    ref = lrb.lr_policy_logp(dev(scores * 0.9), actions)
+    loss, terms, norm = lrb.policy_train_step(t, actions, logp, dev(adv), 1, lr=0.1, max_norm=0.01, weight_decay=0.1,
+                                              ref_logp=ref, **kw)
+    flat = lambda z: z.reshape(s, -1)  # noqa: E731
+    want_lp = ot.policy_logp(scores.reshape(-1, k), flat(want_a))
+    o = ot.policy_loss(scores.reshape(-1, k), flat(want_a), flat(host(logp)), adv, ref_logp=flat(host(ref)),
+                       scale=1.0 / want_a.size, **kw)
+    assert np.allclose(flat(host(logp)), want_lp, atol=1e-5)
+    # (the first step after a draw: every ratio is 1, and the clipped term is minus the advantages' mean)
+    assert abs(float(loss) - o[0]) <= 1e-6 and float(terms[3]) == 0
+    g = host(t._held["d_grad"][0]).reshape(-1, k)
+    assert np.linalg.norm(g - o[2]) <= 2e-5 * np.linalg.norm(o[2])
+    assert abs(float(norm) - ot.grad_norm([g])) <= 1e-6 * ot.grad_norm([g])
+    z = np.zeros(scores.size, np.float32)
+    wp, wm, wv = ot.adamw(scores.reshape(-1), g.reshape(-1), z, z, 1, 0.1, weight_decay=0.1, norm=float(norm),
+                          max_norm=0.01)
+    assert np.allclose(host(x).reshape(-1), wp, rtol=0, atol=1e-5)
+    if bits == 8:
+        cm, cv, sc = ot.encode(wm, wv, ot.random_bits(1, 0, np.arange(z.size)))
+        assert np.array_equal(host(t.m[0]), cm) and np.array_equal(host(t.v[0]), cv)
+
+
+def make_step(lrb, dtype=torch.bfloat16, bits=8):
+    k, s, shape = 32, 6, (3, 33, 35)
+    g = np.random.default_rng([230611268, 44])
+    x = dev(g.standard_normal((*shape, k)).astype(np.float32))
+    bias = dev(g.standard_normal(777).astype(np.float32))
+    t = lrb.TrainTensors([x, bias], [torch.zeros_like(x, dtype=dtype), torch.full_like(bias, 0.01, dtype=dtype)],
+                         bits=bits)
+    noise, levels, adv = dev(gumbel(2, (s, *shape, k))), dev(wl.device_levels(3, k)), dev(
+        g.standard_normal(s).astype(np.float32))
+
+    def step():
+        a, lp, phi = lrb.lr_policy_draw(x, noise, levels)
+        out = lrb.policy_train_step(t, a, lp - 0.05, adv, 3, lr=0.02, ref_logp=lp * 0.98, kl_coef=0.1,
+                                    entropy_coef=0.01, max_norm=0.05)
+        return (a, lp, phi, *out, x, bias, t.m[0], t.v[0])
+
+    return step, (x, bias, *t.m, *t.v, *getattr(t, "scales", []), *t._held["d_grad"])
+
+
+@pytest.mark.parametrize("bits,dtype", [(8, torch.bfloat16), (32, torch.float32)])
+def test_the_recorded_step_replays_as_the_eager_one(lrb, bits, dtype):
+    step, state = make_step(lrb, dtype, bits)
+    start = [z.clone() for z in state]
+    want = []
+    for _ in range(4):
+        want.append([z.clone() for z in step()])
+    for z, z0 in zip(state, start):
+        z.copy_(z0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(z, z0) for z, z0 in zip(state, start))  # (recording runs nothing)
+    for r in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(out, want[r])):
+            assert torch.equal(a, b), (r, i)
+        # eager work of the same kind on other tensors between the replays
+        other, _ = make_step(lrb, dtype, bits)
+        other()
+        torch.cuda.synchronize()
+
+
+def test_another_stream_and_two_at_once(lrb):
+    """Two steps on two streams at the same time, each with its own tensors and workspaces."""
+    (one, s1), (two, s2) = make_step(lrb), make_step(lrb)
+    (ref, s3) = make_step(lrb)
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(a):
+            one()
+        with torch.cuda.stream(b):
+            two()
+        ref()
+    torch.cuda.synchronize()
+    for x, y, z in zip(s1, s2, s3):
+        assert torch.equal(x, z) and torch.equal(y, z)
+
+
+def test_rewards_move_the_policy_towards_the_better_level(lrb):
+    """One pixel row, one level with the larger reward: its score has the only gradient downhill."""
+    k, s = 8, 64
+    x = torch.zeros((5, k), device="cuda")
+    t = lrb.TrainTensors([x], [torch.zeros_like(x)])
+    a, lp, _ = lrb.lr_policy_draw(x, dev(gumbel(3, (s, 5, k))))
+    adv = (a == 3).float()
+    adv = (adv - adv.mean()).contiguous()
+    lrb.policy_train_step(t, a, lp, adv, 1, lr=0.1)
+    g = host(t._held["d_grad"][0])
+    assert np.all(g[:, 3] < 0) and np.all(host(x)[:, 3] > 0)
