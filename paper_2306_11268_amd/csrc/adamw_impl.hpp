@@ -7,7 +7,7 @@
 
 namespace lr {
 
-__device__ __forceinline__ float grad_value(const void* g, long long i, int bf16) {
+__device__ __forceinline__ float grad_at(const void* g, long long i, int bf16) {
   return bf16 ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(g)[i] << 16) : static_cast<const float*>(g)[i];
 }
 
@@ -33,11 +33,11 @@ __global__ void __launch_bounds__(256) grad_norm_kernel(TensorList l, int bf16, 
     const TensorEntry& t = l.t[tensor_of(l, c)];
     for (int j = threadIdx.x; j < kTensorChunk; j += 256) {
       const long long i = (c - t.chunk0) * kTensorChunk + j;
-      const double g = i < t.count ? (double)grad_value(t.grad, i, bf16) : 0.;
+      const double g = i < t.count ? (double)grad_at(t.grad, i, bf16) : 0.;
       s += g * g;
     }
   }
-  s = block_sum_d(s, red);
+  s = block_sum_d<256>(s, red);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(256) grad_norm_finish_kernel(const double* __r
   __shared__ double red[4];
   double s = 0.;
   for (int b = threadIdx.x; b < n; b += 256) s += part[b];
-  s = block_sum_d(s, red);
+  s = block_sum_d<256>(s, red);
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(256) adamw_kernel(TensorList l, AdamwArgs a) {
       float g = 0.f;
       float p = 0.f;
       if (in) {
-        g = grad_value(t.grad, i, a.bf16);
+        g = grad_at(t.grad, i, a.bf16);
         p = t.param[i];
         if (a.bits8) {
           const uint32_t cm = static_cast<const uint8_t*>(t.m)[i];
@@ -121,8 +121,8 @@ __global__ void __launch_bounds__(256) adamw_kernel(TensorList l, AdamwArgs a) {
       }
       if (a.bits8) {
         // (exponents are exact in float32)
-        uint32_t em = (uint32_t)block_max_f((float)((__float_as_uint(m) >> 23) & 255u), redf);
-        uint32_t ev = (uint32_t)block_max_f((float)((__float_as_uint(v) >> 23) & 255u), redf);
+        uint32_t em = (uint32_t)block_reduce<256>((float)((__float_as_uint(m) >> 23) & 255u), OpMax{}, redf);
+        uint32_t ev = (uint32_t)block_reduce<256>((float)((__float_as_uint(v) >> 23) & 255u), OpMax{}, redf);
         em = em < 27u ? 27u : em;
         ev = ev < 27u ? 27u : ev;
         if (in) {

@@ -2,6 +2,8 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <initializer_list>
+#include <type_traits>
 
 #include "adamw_impl.hpp"
 #include "kernels.hpp"

@@ -1,5 +1,12 @@
 // Policy over device levels: levels drawn for several rollouts, their
 // log-probabilities, and the clipped policy loss with its gradient.
+//
+// All three are streaming passes over rows of logits [count][K].  A row of up
+// to kPolicyRowMax levels sits in the registers of G lanes, N values each, as
+// many lanes as keep N at 4 to 16: several rows share a wave, so that the
+// steps of a reduction over lanes serve all of them at once.  A longer row
+// takes a workgroup.  Every logit is read once and its exponential formed
+// once.
 #pragma once
 
 #include "kernels.hpp"
@@ -7,22 +14,115 @@
 
 namespace lr {
 
+constexpr int kPolicyRowMax = 1024;
+constexpr int kPolicyThreads = 256;
+
+// ---- reductions on the vector ALU (no shared memory) -----------------------
+// Lanes 1, 2, 4, 8 apart through DPP (where pairs, quads, ... already agree, the
+// mirrored lane is as good as the one 4 or 8 apart), 16 and 32 apart through
+// the row swaps; every lane of the group ends with the result.
+template <int G, class Op>
+__device__ __forceinline__ float lanes_reduce(float x, Op op) {
+  auto dpp = [&](auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  if constexpr (G >= 2) x = op(x, dpp(std::integral_constant<int, 0xB1>{}));   // quad_perm [1,0,3,2]
+  if constexpr (G >= 4) x = op(x, dpp(std::integral_constant<int, 0x4E>{}));   // quad_perm [2,3,0,1]
+  if constexpr (G >= 8) x = op(x, dpp(std::integral_constant<int, 0x141>{}));  // row_half_mirror
+  if constexpr (G >= 16) x = op(x, dpp(std::integral_constant<int, 0x140>{})); // row_mirror
+  if constexpr (G >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  if constexpr (G >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  }
+  return x;
+}
+struct OpSum {
+  __device__ float operator()(float a, float b) const { return a + b; }
+};
+struct OpMax {
+  __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct OpMin {
+  __device__ float operator()(float a, float b) const { return fminf(a, b); }
+};
+
+template <int G>
+__device__ __forceinline__ double lanes_sum_d(double x) {
+#pragma unroll
+  for (int o = G / 2; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+
+// Over a workgroup of THREADS, in a fixed order; red: THREADS / 64 values.  The
+// last barrier leaves red free for the next call.
+template <int THREADS, class Op>
+__device__ __forceinline__ float block_reduce(float x, Op op, float* red) {
+  x = lanes_reduce<64>(x, op);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = red[0];
+#pragma unroll
+  for (int i = 1; i < THREADS / 64; ++i) x = op(x, red[i]);
+  __syncthreads();
+  return x;
+}
+template <int THREADS>
 __device__ __forceinline__ double block_sum_d(double x, double* red) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) x += __shfl_xor(x, o, 64);
-  __syncthreads();
+  x = lanes_sum_d<64>(x);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
   __syncthreads();
-  return ((red[0] + red[1]) + red[2]) + red[3];
-}
-__device__ __forceinline__ float block_max_f(float x, float* red) {
+  x = red[0];
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+  for (int i = 1; i < THREADS / 64; ++i) x += red[i];
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-  __syncthreads();
-  return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  return x;
 }
+
+// ---- rows in registers -----------------------------------------------------
+// A lane's values are runs of four neighbouring levels: value i of lane l of G
+// is column ((i / 4) G + l) 4 + i % 4.  16-byte loads need only the alignment
+// of one float here, so that rows of any length and place are read alike; TAIL:
+// the last run of a row that is no multiple of four goes value by value.
+struct __attribute__((packed, aligned(4))) Quad {
+  float v[4];
+};
+struct __attribute__((packed, aligned(2))) QuadBf16 {
+  uint32_t v[2];
+};
+template <int G>
+__device__ __forceinline__ int quad_col(int lane, int i) {
+  return ((i / 4) * G + lane) * 4;
+}
+// Columns c .. c + 3 of a row of K; those past the end are `past`.
+template <bool TAIL>
+__device__ __forceinline__ void quad_read(const float* __restrict__ p, int K, int c, float past, float* v) {
+  if (TAIL ? c + 4 <= K : c < K) {
+    const Quad q = *reinterpret_cast<const Quad*>(p + c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = q.v[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = TAIL && j < 3 && c + j < K ? p[c + j] : past;
+  }
+}
+// (K = 0 for a row that is not there)
+template <int G, bool TAIL, int N>
+__device__ __forceinline__ void row_read(const float* __restrict__ p, int K, int lane, float past, float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) quad_read<TAIL>(p, K, quad_col<G>(lane, i), past, &v[i]);
+}
+
+constexpr float kLog2e = 1.44269504088896340736f;
+__device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// Barred levels: far below, but finite, so that 0 times their logarithm is 0.
+// (The maximum drops a NaN; its exponential, formed from the value itself,
+// keeps it.)
+__device__ __forceinline__ float floor_d(float d) { return fmaxf(d, -1e30f); }
 
 __device__ __forceinline__ uint16_t bf16_bits(float x) {
   const uint32_t u = __float_as_uint(x);
@@ -30,166 +130,700 @@ __device__ __forceinline__ uint16_t bf16_bits(float x) {
   return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
 }
 
-// One row per workgroup: the row's log-sum-exp in float64, then its samples.
-__global__ void __launch_bounds__(256) policy_draw_kernel(PolicyDrawArgs a) {
-  __shared__ double red[4];
-  __shared__ float redf[4];
-  __shared__ int best[256];
+// Tile t of the launch's rounds: workgroups of one XCD (every eighth) take
+// neighbouring tiles, whose parts of the [samples][count] arrays share lines.
+__device__ __forceinline__ long long tile_of(long long round, long long tiles) {
+  const unsigned g = gridDim.x;
+  if (g % 8 != 0) return round * g + blockIdx.x;
+  const long long per = (tiles + 7) / 8;  // of one XCD
+  const long long i = round * (g / 8) + blockIdx.x / 8;
+  return i < per ? (blockIdx.x % 8) * per + i : tiles;
+}
+
+// ---- draw ------------------------------------------------------------------
+// One lane of the row's holds the level drawn and its logit, and writes.
+__device__ __forceinline__ void draw_write(const PolicyDrawArgs& a, long long o, int act, float d, float lz) {
+  a.actions[o] = act;
+  if (a.logp) a.logp[o] = d - lz;
+  if (a.phi) a.phi[o] = a.levels[act];
+}
+
+// Best score of this lane's columns and its place: the first of equals (a
+// lane's columns ascend with i); NaN compares false.
+struct Best {
+  float score = -INFINITY;
+  float x = 0.f;
+  int k;
+  __device__ __forceinline__ explicit Best(int K) : k(K) {}
+  __device__ __forceinline__ void take(float xi, float ni, int c) {
+    const float v = xi + ni;
+    const bool better = v > score;
+    score = better ? v : score;
+    k = better ? c : k;
+    x = better ? xi : x;
+  }
+};
+// The row's winner writes (level numbers are exact in float32): top and first
+// are the reductions of all lanes' scores and of the columns that reach it.
+__device__ __forceinline__ void best_write(const PolicyDrawArgs& a, long long o, const Best& b, float top, float first,
+                                           bool lane0, float x0, float m, float lz) {
+  const int act = (int)first;
+  if (act < a.K) {
+    if (b.k == act && b.score == top) draw_write(a, o, act, b.x - m, lz);
+  } else if (lane0) {
+    draw_write(a, o, 0, x0 - m, lz);
+  }
+}
+
+template <int G, int N, bool TAIL>
+__global__ void __launch_bounds__(kPolicyThreads) policy_draw_rows_kernel(PolicyDrawArgs a) {
+  constexpr int T = kPolicyThreads / G;
+  const int lane = threadIdx.x % G;
+  const long long tiles = (a.count + T - 1) / T;
+  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    const long long r = tile * T + threadIdx.x / G;
+    const bool ok = r < a.count;
+    const int K = ok ? a.K : 0;
+    float x[N];
+    row_read<G, TAIL>(a.logits + r * a.K, K, lane, -INFINITY, x);
+    float n[2][N];
+    row_read<G, TAIL>(a.noise + r * a.K, K, lane, 0.f, n[0]);
+    float m = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+    m = lanes_reduce<G>(m, OpMax{});
+    float z = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) z += exp_fast(x[i] - m);
+    const float lz = logf(lanes_reduce<G>(z, OpSum{}));
+    auto one = [&](int s, float (&now)[N], float (&next)[N]) {
+      if (s + 1 < a.samples)
+        row_read<G, TAIL>(a.noise + ((long long)(s + 1) * a.count + r) * a.K, K, lane, 0.f, next);
+      Best b(a.K);
+#pragma unroll
+      for (int i = 0; i < N; ++i) b.take(x[i], now[i], quad_col<G>(lane, i) + i % 4);
+      const float top = lanes_reduce<G>(b.score, OpMax{});
+      const float first = lanes_reduce<G>(b.score == top ? (float)b.k : (float)a.K, OpMin{});
+      if (ok) best_write(a, (long long)s * a.count + r, b, top, first, lane == 0, x[0], m, lz);
+    };
+    for (int s = 0; s < a.samples; s += 2) {
+      one(s, n[0], n[1]);
+      if (s + 1 < a.samples) one(s + 1, n[1], n[0]);
+    }
+  }
+}
+
+// ---- long rows: a workgroup each, streamed -----------------------------------
+// Running maximum, sum of exponentials and of exponential times distance from
+// the maximum; the maximum starts finite, so that barred levels (-inf) leave 0.
+struct Running {
+  float m = -3.402823466e38f;
+  float z = 0.f;
+  float zd = 0.f;
+  __device__ __forceinline__ void rescale(float to) {
+    const float d = m - to;  // <= 0
+    const float f = exp_fast(d);
+    zd = z > 0.f ? f * (zd + d * z) : zd;
+    z *= f;
+    m = to;
+  }
+  template <int N>
+  __device__ __forceinline__ void add(const float (&x)[N]) {
+    float top = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
+    if (top > m) rescale(top);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float d = x[i] - m;
+      const float e = exp_fast(d);
+      z += e;
+      zd += e * floor_d(d);
+    }
+  }
+};
+// Joined over the workgroup: every thread ends with the row's.
+template <int THREADS>
+__device__ __forceinline__ void running_join(Running& w, float* red) {
+  w.rescale(block_reduce<THREADS>(w.m, OpMax{}, red));
+  w.z = block_reduce<THREADS>(w.z, OpSum{}, red);
+  w.zd = block_reduce<THREADS>(w.zd, OpSum{}, red);
+}
+
+constexpr int kLongThreads = 512;
+constexpr int kLongPer = 16;                           // values a thread has in flight
+constexpr int kLongStep = kLongThreads * kLongPer;     // values of a round
+constexpr int kLongSamples = 4;                        // rollouts that one pass over the logits serves
+
+__global__ void __launch_bounds__(kLongThreads) policy_draw_long_kernel(PolicyDrawArgs a) {
+  __shared__ float red[kLongThreads / 64];
+  const int lane = threadIdx.x;
   for (long long r = blockIdx.x; r < a.count; r += gridDim.x) {
-    const float* x = a.logits + r * a.K;
-    float m = -INFINITY;
-    for (int k = threadIdx.x; k < a.K; k += 256) m = fmaxf(m, x[k]);
-    m = block_max_f(m, redf);
-    double z = 0.;
-    for (int k = threadIdx.x; k < a.K; k += 256) z += exp((double)x[k] - (double)m);
-    const double lz = log(block_sum_d(z, red));
-    for (int s = 0; s < a.samples; ++s) {
-      const long long o = (long long)s * a.count + r;
-      int act;
-      if (a.noise) {
-        const float* n = a.noise + o * a.K;
-        float b = -INFINITY;
-        int kb = a.K;
-        for (int k = threadIdx.x; k < a.K; k += 256) {
-          const float v = x[k] + n[k];
-          if (v > b || (v == b && k < kb)) {
-            b = v;
-            kb = k;
-          }
+    const float* __restrict__ row = a.logits + r * a.K;
+    Running w;
+    for (int s0 = 0; s0 < a.samples; s0 += kLongSamples) {
+      Best b[kLongSamples] = {Best(a.K), Best(a.K), Best(a.K), Best(a.K)};
+      for (int k0 = 0; k0 < a.K; k0 += kLongStep) {
+        float x[kLongPer];
+        row_read<kLongThreads, true>(row + k0, a.K - k0, lane, -INFINITY, x);
+#pragma unroll
+        for (int s = 0; s < kLongSamples; ++s) {
+          if (s0 + s >= a.samples) break;
+          float n[kLongPer];
+          row_read<kLongThreads, true>(a.noise + ((long long)(s0 + s) * a.count + r) * a.K + k0, a.K - k0, lane, 0.f, n);
+#pragma unroll
+          for (int i = 0; i < kLongPer; ++i) b[s].take(x[i], n[i], k0 + quad_col<kLongThreads>(lane, i) + i % 4);
         }
-        const float top = block_max_f(b, redf);
-        best[threadIdx.x] = b == top ? kb : a.K;
-        __syncthreads();
-        act = a.K;
-        for (int i = 0; i < 256; ++i) act = best[i] < act ? best[i] : act;
-        if (act >= a.K) act = 0;
-        __syncthreads();
-      } else {
-        act = a.actions[o];
+        if (s0 == 0) w.add(x);
       }
-      if (threadIdx.x == 0) {
-        if (a.noise) a.actions[o] = act;
-        if (a.logp) {
-          float lp = 0.f;
-          if (act >= a.K) lp = __builtin_nanf("");
-          else if (act >= 0) lp = (float)(((double)x[act] - (double)m) - lz);
-          a.logp[o] = lp;
-        }
-        if (a.phi) a.phi[o] = a.levels[act];
+      if (s0 == 0) running_join<kLongThreads>(w, red);
+#pragma unroll
+      for (int s = 0; s < kLongSamples; ++s) {
+        if (s0 + s >= a.samples) break;
+        const float top = block_reduce<kLongThreads>(b[s].score, OpMax{}, red);
+        const float first =
+            block_reduce<kLongThreads>(b[s].score == top ? (float)b[s].k : (float)a.K, OpMin{}, red);
+        best_write(a, (long long)(s0 + s) * a.count + r, b[s], top, first, lane == 0, row[0], w.m, logf(w.z));
       }
     }
   }
 }
 
-__global__ void __launch_bounds__(256) policy_loss_kernel(PolicyLossArgs a) {
-  __shared__ double red[4];
-  __shared__ float redf[4];
-  double t[4] = {0., 0., 0., 0.};
-  const double lo = 1. - (double)a.clip_low;
-  const double hi = 1. + (double)a.clip_high;
+// ---- log-probabilities of given levels ---------------------------------------
+__device__ __forceinline__ float logp_of(const float* __restrict__ row, int act, int K, float m, float lz) {
+  if (act < 0) return 0.f;
+  return act < K ? (row[act] - m) - lz : __builtin_nanf("");
+}
+
+template <int G, int N, bool TAIL>
+__global__ void __launch_bounds__(kPolicyThreads) policy_logp_rows_kernel(PolicyDrawArgs a) {
+  constexpr int T = kPolicyThreads / G;
+  __shared__ float2 stat[T];
+  const int lane = threadIdx.x % G;
+  const int row = threadIdx.x / G;
+  const long long tiles = (a.count + T - 1) / T;
+  for (long long round = 0;; ++round) {
+    const long long tile = tile_of(round, tiles);
+    if (tile >= tiles) return;
+    const long long r0 = tile * T;
+    float x[N];
+    row_read<G, TAIL>(a.logits + (r0 + row) * a.K, r0 + row < a.count ? a.K : 0, lane, -INFINITY, x);
+    float m = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
+    m = lanes_reduce<G>(m, OpMax{});
+    float z = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) z += exp_fast(x[i] - m);
+    z = lanes_reduce<G>(z, OpSum{});
+    if (lane == 0) stat[row] = make_float2(m, logf(z));
+    __syncthreads();
+    for (int q = threadIdx.x; q < a.samples * T; q += kPolicyThreads) {
+      const long long r = r0 + q % T;
+      if (r >= a.count) continue;
+      const long long o = (long long)(q / T) * a.count + r;
+      const float2 t = stat[q % T];
+      a.logp[o] = logp_of(a.logits + r * a.K, a.actions[o], a.K, t.x, t.y);
+    }
+    __syncthreads();
+  }
+}
+
+__global__ void __launch_bounds__(kLongThreads) policy_logp_long_kernel(PolicyDrawArgs a) {
+  __shared__ float red[kLongThreads / 64];
   for (long long r = blockIdx.x; r < a.count; r += gridDim.x) {
-    const float* x = a.logits + r * a.K;
-    float m = -INFINITY;
-    for (int k = threadIdx.x; k < a.K; k += 256) m = fmaxf(m, x[k]);
-    m = block_max_f(m, redf);
-    double z = 0.;
-    double zd = 0.;
-    for (int k = threadIdx.x; k < a.K; k += 256) {
-      const double d = (double)x[k] - (double)m;
-      const double e = exp(d);
-      z += e;
-      if (e > 0.) zd += e * d;
+    const float* __restrict__ row = a.logits + r * a.K;
+    Running w;
+    for (int k0 = 0; k0 < a.K; k0 += kLongStep) {
+      float x[kLongPer];
+      row_read<kLongThreads, true>(row + k0, a.K - k0, threadIdx.x, -INFINITY, x);
+      w.add(x);
     }
-    z = block_sum_d(z, red);
-    const double lz = log(z);
-    const double h = lz - block_sum_d(zd, red) / z;
-    // every thread goes through all choices of the row
-    double g_all = 0.;
-    int made = 0;
-    auto slope = [&](int s, double* terms) {
+    running_join<kLongThreads>(w, red);
+    const float lz = logf(w.z);
+    for (int s = threadIdx.x; s < a.samples; s += kLongThreads) {
       const long long o = (long long)s * a.count + r;
-      const int act = a.actions[o];
-      if (act < 0) return 0.;
-      if (act >= a.K) {
-        terms[0] += __builtin_nan("");
-        terms[1] += __builtin_nan("");
-        terms[2] += __builtin_nan("");
-        terms[3] += __builtin_nan("");
-        return __builtin_nan("");
-      }
-      const double lp = ((double)x[act] - (double)m) - lz;
-      const double ratio = exp(lp - (double)a.old_logp[o]);
-      const double adv = a.per_choice ? a.adv[o] : a.adv[s];
-      const bool cut = adv >= 0. ? ratio > hi : ratio < lo;
-      double g = cut ? 0. : -ratio * adv;
-      terms[0] -= (cut ? (adv >= 0. ? hi : lo) : ratio) * adv;
-      if (a.ref_logp) {
-        const double d = (double)a.ref_logp[o] - lp;
-        terms[1] += expm1(d) - d;
-        g -= (double)a.kl_coef * expm1(d);
-      }
-      terms[2] += h;
-      terms[3] += cut ? 1. : 0.;
-      return g;
-    };
-    double mine[4] = {0., 0., 0., 0.};
-    for (int s = 0; s < a.samples; ++s) {
-      g_all += slope(s, mine);
-      made += a.actions[(long long)s * a.count + r] >= 0;
+      a.logp[o] = logp_of(row, a.actions[o], a.K, w.m, lz);
     }
-    for (int i = 0; i < 4; ++i) t[i] += mine[i];
-    if (a.grad) {
-      for (int k = threadIdx.x; k < a.K; k += 256) {
-        double g = 0.;
-        if (made) {
-          const double d = (double)x[k] - (double)m;
-          const double p = exp(d - lz);
-          g = -p * g_all;
-          if (p > 0.) g += (double)a.entropy_coef * made * p * ((d - lz) + h);
-          double unused[4];
-          for (int s = 0; s < a.samples; ++s)
-            if (a.actions[(long long)s * a.count + r] == k) g += slope(s, unused);
+  }
+}
+
+// ---- the loss ----------------------------------------------------------------
+// One choice of a rollout.
+struct Choice {
+  int act;  // < 0: none
+  float old, ref, adv;
+};
+__device__ __forceinline__ Choice choice_read(const PolicyLossArgs& a, int s, long long r) {
+  const long long o = (long long)s * a.count + r;
+  Choice c;
+  c.act = a.actions[o];
+  c.old = a.old_logp[o];
+  c.ref = a.ref_logp ? a.ref_logp[o] : 0.f;
+  c.adv = a.per_choice ? a.adv[o] : a.adv[s];
+  return c;
+}
+// What the choices of one thread add to the loss's terms.
+struct Terms {
+  float gain = 0.f, kl = 0.f, entropy = 0.f, cut = 0.f;
+};
+// The wave's sums of them, in float32 over its lanes, added to sum in float64.
+__device__ __forceinline__ void terms_add(const Terms& t, double* sum) {
+  const float gain = lanes_reduce<64>(t.gain, OpSum{});
+  const float kl = lanes_reduce<64>(t.kl, OpSum{});
+  const float entropy = lanes_reduce<64>(t.entropy, OpSum{});
+  const float cut = lanes_reduce<64>(t.cut, OpSum{});
+  if ((threadIdx.x & 63) == 0) {
+    sum[0] -= (double)gain;
+    sum[1] += (double)kl;
+    sum[2] += (double)entropy;
+    sum[3] += (double)cut;
+  }
+}
+// The ratio lies so near to its clip border that float32 may put it on the
+// wrong side: the errors of the log-probability (of the level's distance d
+// from the row's maximum, the sum of exponentials and its logarithm) reach over
+// it.  At a border the log-probability is within 90 of old, and |d| within lz
+// of the log-probability.
+__device__ __forceinline__ bool near_border(const PolicyLossArgs& a, const Choice& c, float ratio, float lz) {
+  const float border = c.adv >= 0.f ? 1.f + a.clip_high : 1.f - a.clip_low;
+  return fabsf(ratio - border) <= border * (3.6e-7f * (fabsf(c.old) + lz) + 2.6e-5f);
+}
+// dl/dlogp (times scale) of a choice, its terms added to t.  d: the level's
+// logit minus the row's maximum; lz, h: logarithm of the sum of exponentials
+// and entropy.  side: the clip decision in 64 bits, > 0 over the border, < 0
+// not, 0 not taken.
+__device__ __forceinline__ float choice_slope(const PolicyLossArgs& a, const Choice& c, float d, float ratio, float lz,
+                                              float h, int side, Terms& t) {
+  if (c.act < 0) return 0.f;
+  if (c.act >= a.K) {
+    const float nan = __builtin_nanf("");
+    t.gain = t.kl = t.entropy = t.cut = nan;
+    return nan;
+  }
+  const bool up = c.adv >= 0.f;
+  const float border = up ? 1.f + a.clip_high : 1.f - a.clip_low;
+  const bool cut = side ? side > 0 : (up ? ratio > border : ratio < border);
+  const float g = ratio * c.adv;
+  t.gain += cut ? border * c.adv : g;
+  t.entropy += h;
+  t.cut += cut ? 1.f : 0.f;
+  float slope = cut ? 0.f : -g;
+  if (a.ref_logp) {
+    // e^k - 1 - k: by its series where the difference would cancel
+    const float k = c.ref - (d - lz);
+    float q = 1.f / 3628800;
+    q = q * k + 1.f / 362880;
+    q = q * k + 1.f / 40320;
+    q = q * k + 1.f / 5040;
+    q = q * k + 1.f / 720;
+    q = q * k + 1.f / 120;
+    q = q * k + 1.f / 24;
+    q = q * k + 1.f / 6;
+    q = (q * k + 0.5f) * k * k;
+    if (!(fabsf(k) < 1.f)) q = (exp_fast(k) - 1.f) - k;
+    t.kl += q;
+    if (a.kl_coef != 0.f) slope -= a.kl_coef * (k + q);  // (not 0 times infinity)
+  }
+  return slope * a.scale;
+}
+// e^x for |x| < 700 to about 1e-13: 2^k times the series of the rest, at most
+// ln(2) / 2 (0.35^12 / 12! < 1e-14).  Rolled, its coefficients in memory: the
+// library's function, or the coefficients in registers, would cost every wave
+// of the kernel 40 to 100 registers for a path that few rows take.
+__constant__ double kExpSeries[12] = {1. / 39916800, 1. / 3628800, 1. / 362880, 1. / 40320, 1. / 5040, 1. / 720,
+                                      1. / 120,      1. / 24,      1. / 6,      0.5,        1.,        1.};
+__device__ __forceinline__ double exp_d(double x) {
+  const double k = __builtin_rint(x * 1.4426950408889634074);
+  const double r = __builtin_fma(k, -0.69314718055994530942, x);
+  double p = 0.;
+#pragma unroll 1
+  for (int i = 0; i < 12; ++i) p = __builtin_fma(p, r, kExpSeries[i]);
+  return __builtin_ldexp(p, (int)k);
+}
+// The clip decision in 64 bits: ratio = e^(x - m - old) / z against the border,
+// from the level's logit, the row's maximum and its sum of exponentials.
+__device__ __forceinline__ int side_of(const PolicyLossArgs& a, const Choice& c, float x, float m, double z) {
+  const double u = exp_d(fmin(fmax(((double)x - (double)m) - (double)c.old, -690.), 690.));
+  const bool cut = c.adv >= 0.f ? u > (1. + (double)a.clip_high) * z : u < (1. - (double)a.clip_low) * z;
+  return cut ? 1 : -1;
+}
+// Sum of a row's exponentials in 64 bits, read again from memory by G lanes.
+template <int G>
+__device__ __forceinline__ double sum_exp_d(const float* row, int K, int lane, float m) {
+  double z = 0.;
+#pragma unroll 1
+  for (int k = lane; k < K; k += G) z += exp_d(fmax((double)row[k] - (double)m, -690.));
+  return z;
+}
+__device__ __forceinline__ double wave_sum_exp_d(const float* row, int K, float m) {
+  return lanes_sum_d<64>(sum_exp_d<64>(row, K, threadIdx.x & 63, m));
+}
+// dL/dlogit = (sum of the slopes of choices of this level) - p (all slopes -
+// w (log p + H)), w = scale * entropy_coef * choices made.
+__device__ __forceinline__ float grad_value(float acc, float e, float d, float inv_z, float lz, float h, float slopes,
+                                            float w) {
+  return acc - e * inv_z * (slopes - w * ((d - lz) + h));
+}
+__device__ __forceinline__ void grad_store(void* grad, int bf16, long long at, float g) {
+  if (bf16) static_cast<uint16_t*>(grad)[at] = bf16_bits(g);
+  else static_cast<float*>(grad)[at] = g;
+}
+// Columns c .. c + 3 of a row that starts at `row` in the gradient.
+template <bool TAIL>
+__device__ __forceinline__ void quad_store(void* grad, int bf16, long long row, int K, int c, const float* g) {
+  if (!TAIL || c + 4 <= K) {
+    if (bf16) {
+      const QuadBf16 q{{bf16_bits(g[0]) | (uint32_t)bf16_bits(g[1]) << 16, bf16_bits(g[2]) | (uint32_t)bf16_bits(g[3]) << 16}};
+      *reinterpret_cast<QuadBf16*>(static_cast<uint16_t*>(grad) + row + c) = q;
+    } else {
+      *reinterpret_cast<Quad*>(static_cast<float*>(grad) + row + c) = Quad{{g[0], g[1], g[2], g[3]}};
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 3; ++j)
+      if (c + j < K) grad_store(grad, bf16, row + c + j, g[j]);
+  }
+}
+
+// T rows a workgroup.  1. Their log-sum-exp, in registers; the logits (minus the
+// maximum) also go to shared memory.  2. The choices of all rollouts, a thread
+// each whatever the row's lanes are, read along the rows, find their logits
+// there; their slopes go to shared memory, `chunk` rollouts at a time.  3. A lane
+// per row adds them, one rollout after the other, to the row's levels in
+// shared memory, in the logits' place (the adds of one lane keep their order, so
+// results do not change from run to run, also where rollouts chose the same
+// level).  4. The gradient from registers.
+//
+// The phases wait for each other, so that the pass lives from many workgroups
+// on a CU: nothing is carried from tile to tile but the terms, and the thread's
+// number and K are made new for each, or the compiler holds 70 registers of
+// addresses and comparisons across the loop.  Dynamic shared memory: float
+// [T][K rounded up to four], float2 [chunk][T] (the choices' levels and slopes).
+template <int G, int N, bool TAIL>
+__global__ void __launch_bounds__(kPolicyThreads) policy_loss_rows_kernel(PolicyLossArgs a, int chunk) {
+  constexpr int T = kPolicyThreads / G;
+  extern __shared__ __align__(16) float lds[];
+  __shared__ float2 stat[T];  // log of the sum of exponentials, entropy
+  __shared__ float2 sums[T];  // of the row's slopes and choices
+  __shared__ float stat_m[T];
+  __shared__ double terms[kPolicyThreads / 64][4];  // of each wave
+  if (threadIdx.x < kPolicyThreads / 64 * 4) (&terms[0][0])[threadIdx.x] = 0.;
+  const long long tiles = (a.count + T - 1) / T;
+#pragma unroll 1
+  for (long long round = 0;; ++round) {
+    const long long tile = tile_of(round, tiles);
+    if (tile >= tiles) break;
+    unsigned tid = threadIdx.x;
+    int K = a.K;
+    asm volatile("" : "+v"(tid));
+    asm volatile("" : "+s"(K));
+    const int lane = tid % G;
+    const int row = tid / G;
+    const int stride = (K + 3) / 4 * 4;
+    float2* pairs = reinterpret_cast<float2*>(lds + T * stride);
+    float4* mine = reinterpret_cast<float4*>(lds + row * stride);
+    const long long r0 = tile * T;
+    const bool ok = r0 + row < a.count;
+    float d[N];
+    row_read<G, TAIL>(a.logits + (r0 + row) * K, ok ? K : 0, lane, -INFINITY, d);
+    float m = d[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = fmaxf(m, d[i]);
+    m = lanes_reduce<G>(m, OpMax{});
+    float z = 0.f;
+    float zd = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      d[i] -= m;
+      const float e = exp_fast(d[i]);
+      d[i] = floor_d(d[i]);
+      z += e;
+      zd += e * d[i];
+    }
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const int c = quad_col<G>(lane, i);
+      if (c < K) mine[c / 4] = make_float4(d[i], d[i + 1], d[i + 2], d[i + 3]);
+    }
+    z = lanes_reduce<G>(z, OpSum{});
+    zd = lanes_reduce<G>(zd, OpSum{});
+    const float inv_z = 1.f / z;
+    const float lz = logf(z);
+    const float h = lz - zd * inv_z;
+    if (lane == 0) {
+      stat[row] = make_float2(lz, h);
+      stat_m[row] = m;
+    }
+    float slopes = 0.f;
+    float made = 0.f;
+    __syncthreads();
+    const int mine_row = tid % T;  // whose choices this thread takes
+    const float2 row_stat = stat[mine_row];
+    const float row_m = stat_m[mine_row];
+#pragma unroll 1
+    for (int s0 = 0; s0 < a.samples; s0 += chunk) {
+      const int s1 = min(s0 + chunk, a.samples);
+      Terms add;
+#pragma unroll 1
+      for (int sb = s0; sb < s1; sb += kPolicyThreads / T) {  // (no lane leaves before its wave)
+        const int s = sb + tid / T;
+        Choice c{-1, 0.f, 0.f, 0.f};
+        if (s < s1 && r0 + mine_row < a.count) c = choice_read(a, s, r0 + mine_row);
+        const bool real = (unsigned)c.act < (unsigned)K;
+        float dx = 0.f;
+        if (real)
+          dx = s0 == 0 ? lds[mine_row * stride + c.act] : floor_d(a.logits[(r0 + mine_row) * K + c.act] - row_m);
+        const float ratio = exp_fast((dx - row_stat.x) - c.old);
+        int side = 0;
+        // undecided choices: the wave forms their rows' sums again, in 64 bits
+        for (unsigned long long open = __ballot(real && near_border(a, c, ratio, row_stat.x)); open; open &= open - 1) {
+          const int who = __builtin_ctzll(open);
+          const float* p = a.logits + (r0 + __shfl(mine_row, who, 64)) * K;
+          const double zr = wave_sum_exp_d(p, K, __shfl(row_m, who, 64));
+          if ((int)(threadIdx.x & 63) == who) side = side_of(a, c, p[c.act], row_m, zr);
         }
-        const float gf = (float)(g * (double)a.scale);
-        if (a.bf16) static_cast<uint16_t*>(a.grad)[r * a.K + k] = bf16_bits(gf);
-        else static_cast<float*>(a.grad)[r * a.K + k] = gf;
+        const float g = choice_slope(a, c, dx, ratio, row_stat.x, row_stat.y, side, add);
+        if (s < s1) pairs[(s - s0) * T + mine_row] = make_float2(__int_as_float(c.act < 0 ? -1 : c.act), g);
+      }
+      terms_add(add, terms[tid / 64]);
+      __syncthreads();
+      if (s0 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+          const int c = quad_col<G>(lane, i);
+          if (c < K) mine[c / 4] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        __syncthreads();
+      }
+      if (tid < T) {
+#pragma unroll 4
+        for (int s = 0; s < s1 - s0; ++s) {
+          const float2 c = pairs[s * T + tid];
+          const int act = __float_as_int(c.x);
+          if (act >= 0) {
+            made += 1.f;
+            slopes += c.y;
+            if (act < K)
+              __hip_atomic_fetch_add(&lds[tid * stride + act], c.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+          }
+        }
+        sums[tid] = make_float2(slopes, made);
+      }
+      __syncthreads();
+    }
+    if (a.grad) {
+      const float2 all = sums[row];
+      const float w = a.scale * a.entropy_coef * all.y;
+#pragma unroll
+      for (int i = 0; i < N; i += 4) {
+        const int c = quad_col<G>(lane, i);
+        if (c >= K) continue;
+        const float4 q = mine[c / 4];
+        const float s[4] = {q.x, q.y, q.z, q.w};
+        float g[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          g[j] = all.y > 0.f ? grad_value(s[j], exp_fast(d[i + j]), d[i + j], inv_z, lz, h, all.x, w) : 0.f;
+        if (ok) quad_store<TAIL>(a.grad, a.bf16, (r0 + row) * K, K, c, g);
       }
     }
   }
-  if (threadIdx.x == 0)
-    for (int i = 0; i < 4; ++i) a.part[4 * blockIdx.x + i] = t[i];
+  __syncthreads();
+  if (threadIdx.x < 4) {
+    double s = 0.;
+    for (int w = 0; w < kPolicyThreads / 64; ++w) s += terms[w][threadIdx.x];
+    a.part[4 * blockIdx.x + threadIdx.x] = s;
+  }
+}
+
+// A workgroup per row of more than kPolicyRowMax levels, which is read twice
+// (the second time from the caches): in registers it would leave one workgroup
+// to a CU, whose loads then wait for its own arithmetic.  The gradient is
+// written as if no level had been chosen; then the first rollout that chose a
+// level adds the slopes of all that did, in their order, and writes that value
+// again.
+__global__ void __launch_bounds__(kLongThreads) policy_loss_long_kernel(PolicyLossArgs a) {
+  __shared__ float red[kLongThreads / 64];
+  __shared__ double redd[kLongThreads / 64];
+  __shared__ float2 pairs[1024];  // (as many rollouts as a call may have)
+  const int lane = threadIdx.x;
+  double t[4] = {0., 0., 0., 0.};
+  for (long long r = blockIdx.x; r < a.count; r += gridDim.x) {
+    const float* __restrict__ row = a.logits + r * a.K;
+    Running run;
+    for (int k0 = 0; k0 < a.K; k0 += kLongStep) {
+      float x[kLongPer];
+      row_read<kLongThreads, true>(row + k0, a.K - k0, lane, -INFINITY, x);
+      run.add(x);
+    }
+    running_join<kLongThreads>(run, red);
+    const float m = run.m;
+    const float inv_z = 1.f / run.z;
+    const float lz = logf(run.z);
+    const float h = lz - run.zd * inv_z;
+    bool near = false;
+    Terms add;
+    for (int s = lane; s < a.samples; s += kLongThreads) {
+      const Choice c = choice_read(a, s, r);
+      const bool real = (unsigned)c.act < (unsigned)a.K;
+      const float dx = real ? floor_d(row[c.act] - m) : 0.f;
+      const float ratio = exp_fast((dx - lz) - c.old);
+      const bool here = real && near_border(a, c, ratio, lz);
+      near |= here;
+      // (an undecided choice is left to the second pass)
+      const float g = here ? 0.f : choice_slope(a, c, dx, ratio, lz, h, 0, add);
+      pairs[s] = make_float2(__int_as_float(here ? -2 : (c.act < 0 ? -1 : c.act)), g);
+    }
+    if (__syncthreads_or(near)) {
+      const double zr = block_sum_d<kLongThreads>(sum_exp_d<kLongThreads>(row, a.K, lane, m), redd);
+      for (int s = lane; s < a.samples; s += kLongThreads) {
+        if (__float_as_int(pairs[s].x) != -2) continue;
+        const Choice c = choice_read(a, s, r);
+        const float x = row[c.act];
+        const float g = choice_slope(a, c, x - m, exp_fast((x - m - lz) - c.old), lz, h, side_of(a, c, x, m, zr), add);
+        pairs[s] = make_float2(__int_as_float(c.act), g);
+      }
+      __syncthreads();
+    }
+    t[0] -= (double)add.gain;
+    t[1] += (double)add.kl;
+    t[2] += (double)add.entropy;
+    t[3] += (double)add.cut;
+    if (a.grad) {
+      float slopes = 0.f;
+      float made = 0.f;
+      for (int s = 0; s < a.samples; ++s) {
+        const float2 c = pairs[s];
+        if (__float_as_int(c.x) >= 0) {
+          made += 1.f;
+          slopes += c.y;
+        }
+      }
+      const float w = a.scale * a.entropy_coef * made;
+      for (int k0 = 0; k0 < a.K; k0 += kLongStep) {
+        float x[kLongPer];
+        row_read<kLongThreads, true>(row + k0, a.K - k0, lane, -INFINITY, x);
+#pragma unroll
+        for (int i = 0; i < kLongPer; ++i) {
+          const float d = x[i] - m;
+          x[i] = made > 0.f ? grad_value(0.f, exp_fast(d), floor_d(d), inv_z, lz, h, slopes, w) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < kLongPer; i += 4)
+          quad_store<true>(a.grad, a.bf16, r * a.K, a.K, k0 + quad_col<kLongThreads>(lane, i), &x[i]);
+      }
+      __syncthreads();  // (the row's stores come before those below)
+      for (int s = lane; s < a.samples; s += kLongThreads) {
+        const int act = __float_as_int(pairs[s].x);
+        if (act < 0 || act >= a.K) continue;
+        float g = 0.f;
+        bool first = true;
+        for (int o = 0; o < a.samples; ++o) {
+          const float2 c = pairs[o];
+          if (__float_as_int(c.x) != act) continue;
+          first &= o >= s;
+          g += c.y;
+        }
+        if (!first) continue;
+        const float d = row[act] - m;
+        grad_store(a.grad, a.bf16, r * a.K + act, grad_value(g, exp_fast(d), floor_d(d), inv_z, lz, h, slopes, w));
+      }
+    }
+    __syncthreads();
+  }
+  for (int i = 0; i < 4; ++i) {
+    const double s = block_sum_d<kLongThreads>(t[i], redd);
+    if (threadIdx.x == 0) a.part[4 * blockIdx.x + i] = s;
+  }
 }
 
 // The loss and its four terms from the workgroups' partial sums.
 __global__ void __launch_bounds__(256) policy_finish_kernel(const double* __restrict__ part, int n, float kl, float ent,
                                                             float scale, float* loss, float* terms) {
   __shared__ double red[4];
-  double t[4];
-  for (int i = 0; i < 4; ++i) {
-    double s = 0.;
-    for (int b = threadIdx.x; b < n; b += 256) s += part[4 * b + i];
-    t[i] = block_sum_d(s, red) * (double)scale;
-  }
+  double t[4] = {0., 0., 0., 0.};
+  for (int b = threadIdx.x; b < n; b += 256)
+    for (int i = 0; i < 4; ++i) t[i] += part[4 * b + i];
+  for (int i = 0; i < 4; ++i) t[i] = block_sum_d<256>(t[i], red) * (double)scale;
   if (threadIdx.x == 0) {
-    if (loss) *loss = (float)(t[0] + (double)kl * t[1] - (double)ent * t[2]);
+    if (loss) *loss = (float)(t[0] + (kl != 0.f ? (double)kl * t[1] : 0.) - (double)ent * t[2]);
     if (terms)
       for (int i = 0; i < 4; ++i) terms[i] = (float)t[i];
   }
 }
 
+// ---- launches ------------------------------------------------------------------
+// Calls rows(Shape<G, N, TAIL>) for K <= kPolicyRowMax levels, else longs().
+template <int G_, int N_, bool TAIL_>
+struct Shape {
+  static constexpr int G = G_, N = N_;
+  static constexpr bool TAIL = TAIL_;
+};
+template <bool TAIL, class F>
+static void policy_rows_shape(int K, F&& rows) {
+  if (K <= 4) rows(Shape<1, 4, TAIL>{});
+  else if (K <= 8) rows(Shape<2, 4, TAIL>{});
+  else if (K <= 16) rows(Shape<4, 4, TAIL>{});
+  else if (K <= 32) rows(Shape<4, 8, TAIL>{});
+  else if (K <= 64) rows(Shape<8, 8, TAIL>{});
+  else if (K <= 128) rows(Shape<8, 16, TAIL>{});
+  else if (K <= 256) rows(Shape<16, 16, TAIL>{});
+  else if (K <= 512) rows(Shape<32, 16, TAIL>{});
+  else rows(Shape<64, 16, TAIL>{});
+}
+template <class F, class L>
+static void policy_shape(int K, F&& rows, L&& longs) {
+  if (K > kPolicyRowMax) longs();
+  else if (K % 4) policy_rows_shape<true>(K, rows);
+  else policy_rows_shape<false>(K, rows);
+}
+template <int G>
+static dim3 policy_grid(long long count, long long most) {
+  const long long tiles = (count + kPolicyThreads / G - 1) / (kPolicyThreads / G);
+  return dim3((unsigned)std::min(tiles, most));
+}
+
 hipError_t launch_policy_draw(const PolicyDrawArgs& a, hipStream_t st) {
   if (a.count <= 0 || a.samples <= 0) return hipSuccess;
-  const unsigned grid = (unsigned)std::min<long long>(a.count, 1 << 20);
-  hipLaunchKernelGGL(policy_draw_kernel, dim3(grid), dim3(256), 0, st, a);
+  policy_shape(
+      a.K,
+      [&](auto s) {
+        using S = decltype(s);
+        const dim3 grid = policy_grid<S::G>(a.count, 1 << 16);
+        if (a.noise) hipLaunchKernelGGL((policy_draw_rows_kernel<S::G, S::N, S::TAIL>), grid, dim3(kPolicyThreads), 0, st, a);
+        else hipLaunchKernelGGL((policy_logp_rows_kernel<S::G, S::N, S::TAIL>), grid, dim3(kPolicyThreads), 0, st, a);
+      },
+      [&] {
+        const dim3 grid((unsigned)std::min<long long>(a.count, 1 << 16));
+        if (a.noise) hipLaunchKernelGGL(policy_draw_long_kernel, grid, dim3(kLongThreads), 0, st, a);
+        else hipLaunchKernelGGL(policy_logp_long_kernel, grid, dim3(kLongThreads), 0, st, a);
+      });
   return hipGetLastError();
 }
 
 hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) {
   if (a.count <= 0 || a.samples <= 0) return hipSuccess;
-  const unsigned grid = (unsigned)std::min<long long>(a.count, kPolicyParts);
-  hipLaunchKernelGGL(policy_loss_kernel, dim3(grid), dim3(256), 0, st, a);
+  dim3 grid;
+  policy_shape(
+      a.K,
+      [&](auto s) {
+        using S = decltype(s);
+        constexpr int T = kPolicyThreads / S::G;
+        // levels (at most 16 KB) and choices in what lets eight workgroups share a CU's 160 KB
+        const size_t table = (size_t)T * ((a.K + 3) / 4 * 4) * 4;
+        const int fit = (int)((20480 - 64 - 20 * T - (int)table) / (8 * T));
+        const int chunk = std::max(1, std::min(a.samples, fit));
+        const size_t lds = table + (size_t)chunk * T * 8;
+        grid = policy_grid<S::G>(a.count, kPolicyParts);
+        hipLaunchKernelGGL((policy_loss_rows_kernel<S::G, S::N, S::TAIL>), grid, dim3(kPolicyThreads), lds, st, a, chunk);
+      },
+      [&] {
+        grid = dim3((unsigned)std::min<long long>(a.count, kPolicyParts));
+        hipLaunchKernelGGL(policy_loss_long_kernel, grid, dim3(kLongThreads), 0, st, a);
+      });
   if (a.loss || a.terms)
-    hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(256), 0, st, a.part, (int)grid, a.kl_coef, a.entropy_coef,
+    hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(256), 0, st, a.part, (int)grid.x, a.kl_coef, a.entropy_coef,
                        a.scale, a.loss, a.terms);
   return hipGetLastError();
 }
