@@ -354,8 +354,8 @@ struct Choice {
   int act;  // < 0: none
   float old, ref, adv;
 };
-__device__ __forceinline__ Choice choice_read(const PolicyLossArgs& a, int s, long long r) {
-  const long long o = (long long)s * a.count + r;
+// Rollout s, place o of the [samples][count] arrays.
+__device__ __forceinline__ Choice choice_read(const PolicyLossArgs& a, int s, long long o) {
   Choice c;
   c.act = a.actions[o];
   c.old = a.old_logp[o];
@@ -380,38 +380,43 @@ __device__ __forceinline__ void terms_add(const Terms& t, double* sum) {
     sum[3] += (double)cut;
   }
 }
-// The ratio lies so near to its clip border that float32 may put it on the
-// wrong side: the errors of the log-probability (of the level's distance d
-// from the row's maximum, the sum of exponentials and its logarithm) reach over
-// it.  At a border the log-probability is within 90 of old, and |d| within lz
-// of the log-probability.
-__device__ __forceinline__ bool near_border(const PolicyLossArgs& a, const Choice& c, float ratio, float lz) {
-  const float border = c.adv >= 0.f ? 1.f + a.clip_high : 1.f - a.clip_low;
-  return fabsf(ratio - border) <= border * (3.6e-7f * (fabsf(c.old) + lz) + 2.6e-5f);
-}
-// dl/dlogp (times scale) of a choice, its terms added to t.  d: the level's
-// logit minus the row's maximum; lz, h: logarithm of the sum of exponentials
-// and entropy.  side: the clip decision in 64 bits, > 0 over the border, < 0
-// not, 0 not taken.
-__device__ __forceinline__ float choice_slope(const PolicyLossArgs& a, const Choice& c, float d, float ratio, float lz,
-                                              float h, int side, Terms& t) {
-  if (c.act < 0) return 0.f;
-  if (c.act >= a.K) {
-    const float nan = __builtin_nanf("");
-    t.gain = t.kl = t.entropy = t.cut = nan;
-    return nan;
+// A choice under the present logits.  d: its level's logit minus the row's
+// maximum, NaN for a level out of range.
+struct Ratio {
+  float logp, ratio, border;
+  float over;  // > 0: on the clipped side
+  __device__ __forceinline__ Ratio(const PolicyLossArgs& a, const Choice& c, float d, float lz) {
+    logp = d - lz;
+    ratio = exp_fast(logp - c.old);
+    const bool up = c.adv >= 0.f;
+    border = up ? 1.f + a.clip_high : 1.f - a.clip_low;
+    over = up ? ratio - border : border - ratio;
   }
-  const bool up = c.adv >= 0.f;
-  const float border = up ? 1.f + a.clip_high : 1.f - a.clip_low;
-  const bool cut = side ? side > 0 : (up ? ratio > border : ratio < border);
-  const float g = ratio * c.adv;
-  t.gain += cut ? border * c.adv : g;
-  t.entropy += h;
-  t.cut += cut ? 1.f : 0.f;
+  // So near to the border that float32 may put it on the wrong side: the errors
+  // of the log-probability (of d, the sum of exponentials and its logarithm)
+  // reach over it.  There the log-probability is within 90 of old, and |d|
+  // within lz of the log-probability.
+  __device__ __forceinline__ bool open(const Choice& c, float lz) const {
+    return fabsf(over) <= border * (3.6e-7f * (fabsf(c.old) + lz) + 2.6e-5f);
+  }
+};
+// dl/dlogp (times scale) of a choice, its terms added to t; h: the row's
+// entropy.  Without branches: a place without a choice (whose numbers may be
+// anything) is left out at the end.
+__device__ __forceinline__ float choice_slope(const PolicyLossArgs& a, const Choice& c, const Ratio& r, float h,
+                                              Terms& t) {
+  const bool made = c.act >= 0;
+  const bool real = c.act < a.K;
+  const bool cut = r.over > 0.f;
+  const float g = r.ratio * c.adv;
+  const float gain = cut ? r.border * c.adv : g;
   float slope = cut ? 0.f : -g;
+  t.gain += made ? gain : 0.f;
+  t.entropy += made ? (real ? h : __builtin_nanf("")) : 0.f;
+  t.cut += made ? (cut ? 1.f : real ? 0.f : __builtin_nanf("")) : 0.f;
   if (a.ref_logp) {
     // e^k - 1 - k: by its series where the difference would cancel
-    const float k = c.ref - (d - lz);
+    const float k = c.ref - r.logp;
     float q = 1.f / 3628800;
     q = q * k + 1.f / 362880;
     q = q * k + 1.f / 40320;
@@ -422,10 +427,10 @@ __device__ __forceinline__ float choice_slope(const PolicyLossArgs& a, const Cho
     q = q * k + 1.f / 6;
     q = (q * k + 0.5f) * k * k;
     if (!(fabsf(k) < 1.f)) q = (exp_fast(k) - 1.f) - k;
-    t.kl += q;
+    t.kl += made ? q : 0.f;
     if (a.kl_coef != 0.f) slope -= a.kl_coef * (k + q);  // (not 0 times infinity)
   }
-  return slope * a.scale;
+  return made ? slope * a.scale : 0.f;
 }
 // e^x for |x| < 700 to about 1e-13: 2^k times the series of the rest, at most
 // ln(2) / 2 (0.35^12 / 12! < 1e-14).  Rolled, its coefficients in memory: the
@@ -441,12 +446,11 @@ __device__ __forceinline__ double exp_d(double x) {
   for (int i = 0; i < 12; ++i) p = __builtin_fma(p, r, kExpSeries[i]);
   return __builtin_ldexp(p, (int)k);
 }
-// The clip decision in 64 bits: ratio = e^(x - m - old) / z against the border,
-// from the level's logit, the row's maximum and its sum of exponentials.
-__device__ __forceinline__ int side_of(const PolicyLossArgs& a, const Choice& c, float x, float m, double z) {
+// Ratio::over in 64 bits, times z: ratio = e^(x - m - old) / z against the
+// border, from the level's logit, the row's maximum and its sum of exponentials.
+__device__ __forceinline__ float over_d(const PolicyLossArgs& a, const Choice& c, float x, float m, double z) {
   const double u = exp_d(fmin(fmax(((double)x - (double)m) - (double)c.old, -690.), 690.));
-  const bool cut = c.adv >= 0.f ? u > (1. + (double)a.clip_high) * z : u < (1. - (double)a.clip_low) * z;
-  return cut ? 1 : -1;
+  return (float)(c.adv >= 0.f ? u - (1. + (double)a.clip_high) * z : (1. - (double)a.clip_low) * z - u);
 }
 // Sum of a row's exponentials in 64 bits, read again from memory by G lanes.
 template <int G>
@@ -489,23 +493,35 @@ __device__ __forceinline__ void quad_store(void* grad, int bf16, long long row, 
 // T rows a workgroup.  1. Their log-sum-exp, in registers; the logits (minus the
 // maximum) also go to shared memory.  2. The choices of all rollouts, a thread
 // each whatever the row's lanes are, read along the rows, find their logits
-// there; their slopes go to shared memory, `chunk` rollouts at a time.  3. A lane
-// per row adds them, one rollout after the other, to the row's levels in
-// shared memory, in the logits' place (the adds of one lane keep their order, so
+// there.  Their slopes are added to the row's levels in shared memory, by one
+// lane in the order of the rollouts (the adds of one lane keep their order, so
 // results do not change from run to run, also where rollouts chose the same
-// level).  4. The gradient from registers.
+// level).  3. The gradient from registers.
+//
+// DIRECT, rows of few levels: the thread that forms a slope adds it, into one of
+// the G tables that the threads of a row have; the gradient joins the tables.
+// Otherwise the choices' levels and slopes go to shared memory, `chunk` rollouts
+// at a time, and a lane per row adds them in the logits' place.  (612500 rows of
+// 16 levels, 32 rollouts: 165 us through the list, whose one adding wave the
+// others wait for.)
 //
 // The phases wait for each other, so that the pass lives from many workgroups
 // on a CU: nothing is carried from tile to tile but the terms, and the thread's
 // number and K are made new for each, or the compiler holds 70 registers of
-// addresses and comparisons across the loop.  Dynamic shared memory: float
-// [T][K rounded up to four], float2 [chunk][T] (the choices' levels and slopes).
+// addresses and comparisons across the loop.  Dynamic shared memory (K rounded
+// up to four): DIRECT float [1 + G][T][K], the logits first; else float [T][K]
+// and float2 [chunk][T].
+template <int G, int N>
+constexpr bool kDirect = G * N <= 32;
+
 template <int G, int N, bool TAIL>
 __global__ void __launch_bounds__(kPolicyThreads) policy_loss_rows_kernel(PolicyLossArgs a, int chunk) {
+  constexpr bool DIRECT = kDirect<G, N>;
   constexpr int T = kPolicyThreads / G;
+  constexpr int PARTS = DIRECT ? G : 1;
   extern __shared__ __align__(16) float lds[];
-  __shared__ float2 stat[T];  // log of the sum of exponentials, entropy
-  __shared__ float2 sums[T];  // of the row's slopes and choices
+  __shared__ float2 stat[T];         // log of the sum of exponentials, entropy
+  __shared__ float2 sums[PARTS][T];  // of the row's slopes and choices
   __shared__ float stat_m[T];
   __shared__ double terms[kPolicyThreads / 64][4];  // of each wave
   if (threadIdx.x < kPolicyThreads / 64 * 4) (&terms[0][0])[threadIdx.x] = 0.;
@@ -521,10 +537,20 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_loss_rows_kernel(Policy
     const int lane = tid % G;
     const int row = tid / G;
     const int stride = (K + 3) / 4 * 4;
-    float2* pairs = reinterpret_cast<float2*>(lds + T * stride);
+    const int table = T * stride;
+    float2* pairs = reinterpret_cast<float2*>(lds + table);
     float4* mine = reinterpret_cast<float4*>(lds + row * stride);
     const long long r0 = tile * T;
     const bool ok = r0 + row < a.count;
+    const int part = tid / T;
+    const int mine_row = tid % T;  // whose choices this thread takes, G rollouts apart
+    long long at = part * a.count + r0 + mine_row;
+    auto fetch = [&](int s, long long o) {
+      Choice c{-1, 0.f, 0.f, 0.f};
+      if (s < a.samples && r0 + mine_row < a.count) c = choice_read(a, s, o);
+      return c;
+    };
+    Choice next = fetch(part, at);
     float d[N];
     row_read<G, TAIL>(a.logits + (r0 + row) * K, ok ? K : 0, lane, -INFINITY, d);
     float m = d[0];
@@ -544,7 +570,12 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_loss_rows_kernel(Policy
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
       const int c = quad_col<G>(lane, i);
-      if (c < K) mine[c / 4] = make_float4(d[i], d[i + 1], d[i + 2], d[i + 3]);
+      if (c >= K) continue;
+      mine[c / 4] = make_float4(d[i], d[i + 1], d[i + 2], d[i + 3]);
+      if (DIRECT) {
+#pragma unroll
+        for (int p = 1; p <= PARTS; ++p) mine[p * (table / 4) + c / 4] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
     }
     z = lanes_reduce<G>(z, OpSum{});
     zd = lanes_reduce<G>(zd, OpSum{});
@@ -557,69 +588,89 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_loss_rows_kernel(Policy
     }
     float slopes = 0.f;
     float made = 0.f;
+    Terms add;
     __syncthreads();
-    const int mine_row = tid % T;  // whose choices this thread takes
     const float2 row_stat = stat[mine_row];
     const float row_m = stat_m[mine_row];
-#pragma unroll 1
-    for (int s0 = 0; s0 < a.samples; s0 += chunk) {
-      const int s1 = min(s0 + chunk, a.samples);
-      Terms add;
-#pragma unroll 1
-      for (int sb = s0; sb < s1; sb += kPolicyThreads / T) {  // (no lane leaves before its wave)
-        const int s = sb + tid / T;
-        Choice c{-1, 0.f, 0.f, 0.f};
-        if (s < s1 && r0 + mine_row < a.count) c = choice_read(a, s, r0 + mine_row);
-        const bool real = (unsigned)c.act < (unsigned)K;
-        float dx = 0.f;
-        if (real)
-          dx = s0 == 0 ? lds[mine_row * stride + c.act] : floor_d(a.logits[(r0 + mine_row) * K + c.act] - row_m);
-        const float ratio = exp_fast((dx - row_stat.x) - c.old);
-        int side = 0;
-        // undecided choices: the wave forms their rows' sums again, in 64 bits
-        for (unsigned long long open = __ballot(real && near_border(a, c, ratio, row_stat.x)); open; open &= open - 1) {
-          const int who = __builtin_ctzll(open);
-          const float* p = a.logits + (r0 + __shfl(mine_row, who, 64)) * K;
-          const double zr = wave_sum_exp_d(p, K, __shfl(row_m, who, 64));
-          if ((int)(threadIdx.x & 63) == who) side = side_of(a, c, p[c.act], row_m, zr);
-        }
-        const float g = choice_slope(a, c, dx, ratio, row_stat.x, row_stat.y, side, add);
-        if (s < s1) pairs[(s - s0) * T + mine_row] = make_float2(__int_as_float(c.act < 0 ? -1 : c.act), g);
+    const float* row_d = lds + mine_row * stride;
+    float* row_add = lds + (DIRECT ? (1 + part) * table : 0) + mine_row * stride;
+    // (a tail of the row's choices: no lane leaves before its wave)
+    auto choose = [&](int s, bool near_lds) {
+      const Choice c = next;
+      at += G * a.count;
+      next = fetch(s + G, at);
+      const bool real = (unsigned)c.act < (unsigned)K;
+      float dx;
+      if (near_lds) dx = row_d[real ? c.act : 0];
+      else dx = floor_d(a.logits[real ? (r0 + mine_row) * K + c.act : 0] - row_m);
+      Ratio ratio(a, c, c.act < K ? dx : __builtin_nanf(""), row_stat.x);
+      // undecided choices: the wave forms their rows' sums again, in 64 bits
+      for (unsigned long long open = __ballot(real && ratio.open(c, row_stat.x)); open; open &= open - 1) {
+        const int who = __builtin_ctzll(open);
+        const float* p = a.logits + (r0 + __shfl(mine_row, who, 64)) * K;
+        const double zr = wave_sum_exp_d(p, K, __shfl(row_m, who, 64));
+        if ((int)(threadIdx.x & 63) == who) ratio.over = over_d(a, c, p[c.act], row_m, zr);
       }
-      terms_add(add, terms[tid / 64]);
-      __syncthreads();
-      if (s0 == 0) {
-#pragma unroll
-        for (int i = 0; i < N; i += 4) {
-          const int c = quad_col<G>(lane, i);
-          if (c < K) mine[c / 4] = make_float4(0.f, 0.f, 0.f, 0.f);
+      return make_float2(__int_as_float(c.act), choice_slope(a, c, ratio, row_stat.y, add));
+    };
+    auto collect = [&](float2 c) {
+      const int act = __float_as_int(c.x);
+      if (act >= 0) {
+        made += 1.f;
+        slopes += c.y;
+        if (act < K) __hip_atomic_fetch_add(row_add + act, c.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+      }
+    };
+    if constexpr (DIRECT) {
+#pragma unroll 1
+      for (int s = 0; s < a.samples; s += G) collect(choose(s + part, true));
+      sums[part][mine_row] = make_float2(slopes, made);
+    } else {
+#pragma unroll 1
+      for (int s0 = 0; s0 < a.samples; s0 += chunk) {
+        const int s1 = min(s0 + chunk, a.samples);
+#pragma unroll 1
+        for (int s = s0; s < s1; s += G) {
+          const float2 c = choose(s + part, s0 == 0);
+          if (s + part < s1) pairs[(s + part - s0) * T + mine_row] = c;
         }
         __syncthreads();
-      }
-      if (tid < T) {
-#pragma unroll 4
-        for (int s = 0; s < s1 - s0; ++s) {
-          const float2 c = pairs[s * T + tid];
-          const int act = __float_as_int(c.x);
-          if (act >= 0) {
-            made += 1.f;
-            slopes += c.y;
-            if (act < K)
-              __hip_atomic_fetch_add(&lds[tid * stride + act], c.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        if (s0 == 0) {
+#pragma unroll
+          for (int i = 0; i < N; i += 4) {
+            const int c = quad_col<G>(lane, i);
+            if (c < K) mine[c / 4] = make_float4(0.f, 0.f, 0.f, 0.f);
           }
+          __syncthreads();
         }
-        sums[tid] = make_float2(slopes, made);
+        if (tid < T) {
+#pragma unroll 4
+          for (int s = 0; s < s1 - s0; ++s) collect(pairs[s * T + mine_row]);
+          sums[0][mine_row] = make_float2(slopes, made);
+        }
+        if (s1 < a.samples) __syncthreads();
       }
-      __syncthreads();
     }
+    terms_add(add, terms[tid / 64]);
+    __syncthreads();
     if (a.grad) {
-      const float2 all = sums[row];
+      float2 all = sums[0][row];
+#pragma unroll
+      for (int p = 1; p < PARTS; ++p) {
+        all.x += sums[p][row].x;
+        all.y += sums[p][row].y;
+      }
       const float w = a.scale * a.entropy_coef * all.y;
 #pragma unroll
       for (int i = 0; i < N; i += 4) {
         const int c = quad_col<G>(lane, i);
         if (c >= K) continue;
-        const float4 q = mine[c / 4];
+        float4 q = mine[(DIRECT ? table / 4 : 0) + c / 4];
+#pragma unroll
+        for (int p = 2; p <= PARTS; ++p) {
+          const float4 o = mine[p * (table / 4) + c / 4];
+          q = make_float4(q.x + o.x, q.y + o.y, q.z + o.z, q.w + o.w);
+        }
         const float s[4] = {q.x, q.y, q.z, q.w};
         float g[4];
 #pragma unroll
@@ -665,23 +716,24 @@ __global__ void __launch_bounds__(kLongThreads) policy_loss_long_kernel(PolicyLo
     bool near = false;
     Terms add;
     for (int s = lane; s < a.samples; s += kLongThreads) {
-      const Choice c = choice_read(a, s, r);
+      const Choice c = choice_read(a, s, (long long)s * a.count + r);
       const bool real = (unsigned)c.act < (unsigned)a.K;
-      const float dx = real ? floor_d(row[c.act] - m) : 0.f;
-      const float ratio = exp_fast((dx - lz) - c.old);
-      const bool here = real && near_border(a, c, ratio, lz);
+      const Ratio ratio(a, c, real ? floor_d(row[c.act] - m) : __builtin_nanf(""), lz);
+      const bool here = real && ratio.open(c, lz);
       near |= here;
       // (an undecided choice is left to the second pass)
-      const float g = here ? 0.f : choice_slope(a, c, dx, ratio, lz, h, 0, add);
+      const float g = here ? 0.f : choice_slope(a, c, ratio, h, add);
       pairs[s] = make_float2(__int_as_float(here ? -2 : (c.act < 0 ? -1 : c.act)), g);
     }
     if (__syncthreads_or(near)) {
       const double zr = block_sum_d<kLongThreads>(sum_exp_d<kLongThreads>(row, a.K, lane, m), redd);
       for (int s = lane; s < a.samples; s += kLongThreads) {
         if (__float_as_int(pairs[s].x) != -2) continue;
-        const Choice c = choice_read(a, s, r);
+        const Choice c = choice_read(a, s, (long long)s * a.count + r);
         const float x = row[c.act];
-        const float g = choice_slope(a, c, x - m, exp_fast((x - m - lz) - c.old), lz, h, side_of(a, c, x, m, zr), add);
+        Ratio ratio(a, c, x - m, lz);
+        ratio.over = over_d(a, c, x, m, zr);
+        const float g = choice_slope(a, c, ratio, h, add);
         pairs[s] = make_float2(__int_as_float(c.act), g);
       }
       __syncthreads();
@@ -810,11 +862,13 @@ hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) {
       [&](auto s) {
         using S = decltype(s);
         constexpr int T = kPolicyThreads / S::G;
-        // levels (at most 16 KB) and choices in what lets eight workgroups share a CU's 160 KB
-        const size_t table = (size_t)T * ((a.K + 3) / 4 * 4) * 4;
-        const int fit = (int)((20480 - 64 - 20 * T - (int)table) / (8 * T));
-        const int chunk = std::max(1, std::min(a.samples, fit));
-        const size_t lds = table + (size_t)chunk * T * 8;
+        const int table = T * ((a.K + 3) / 4 * 4) * 4;
+        // (the list: a whole number of the kernel's rounds of kPolicyThreads choices, in what leaves eight
+        // workgroups to a CU's 160 KB beside at most 16 KB of levels)
+        const int fit = (20480 - 192 - 20 * T - table) / (8 * kPolicyThreads);
+        const int rounds = (a.samples + S::G - 1) / S::G;
+        const int chunk = std::max(1, std::min(rounds, fit)) * S::G;
+        const size_t lds = kDirect<S::G, S::N> ? (size_t)table * (1 + S::G) : table + (size_t)chunk * T * 8;
         grid = policy_grid<S::G>(a.count, kPolicyParts);
         hipLaunchKernelGGL((policy_loss_rows_kernel<S::G, S::N, S::TAIL>), grid, dim3(kPolicyThreads), lds, st, a, chunk);
       },
