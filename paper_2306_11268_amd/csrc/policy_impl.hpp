@@ -16,6 +16,7 @@ namespace lr {
 
 constexpr int kPolicyRowMax = 1024;
 constexpr int kPolicyThreads = 256;
+constexpr int kPolicyCus = 256;  // of the MI355X
 
 // ---- reductions on the vector ALU (no shared memory) -----------------------
 // Lanes 1, 2, 4, 8 apart through DPP (where pairs, quads, ... already agree, the
@@ -128,16 +129,6 @@ __device__ __forceinline__ uint16_t bf16_bits(float x) {
   const uint32_t u = __float_as_uint(x);
   if ((u & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((u >> 16) | 0x40);  // (a NaN stays one)
   return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
-}
-
-// Tile t of the launch's rounds: workgroups of one XCD (every eighth) take
-// neighbouring tiles, whose parts of the [samples][count] arrays share lines.
-__device__ __forceinline__ long long tile_of(long long round, long long tiles) {
-  const unsigned g = gridDim.x;
-  if (g % 8 != 0) return round * g + blockIdx.x;
-  const long long per = (tiles + 7) / 8;  // of one XCD
-  const long long i = round * (g / 8) + blockIdx.x / 8;
-  return i < per ? (blockIdx.x % 8) * per + i : tiles;
 }
 
 // ---- draw ------------------------------------------------------------------
@@ -302,9 +293,7 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_logp_rows_kernel(Policy
   const int lane = threadIdx.x % G;
   const int row = threadIdx.x / G;
   const long long tiles = (a.count + T - 1) / T;
-  for (long long round = 0;; ++round) {
-    const long long tile = tile_of(round, tiles);
-    if (tile >= tiles) return;
+  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     const long long r0 = tile * T;
     float x[N];
     row_read<G, TAIL>(a.logits + (r0 + row) * a.K, r0 + row < a.count ? a.K : 0, lane, -INFINITY, x);
@@ -354,13 +343,14 @@ struct Choice {
   int act;  // < 0: none
   float old, ref, adv;
 };
-// Rollout s, place o of the [samples][count] arrays.
-__device__ __forceinline__ Choice choice_read(const PolicyLossArgs& a, int s, long long o) {
+// Rollout s, place o + k of the [samples][count] arrays (o in scalar registers
+// where the whole wave shares it).
+__device__ __forceinline__ Choice choice_read(const PolicyLossArgs& a, int s, long long o, unsigned k) {
   Choice c;
-  c.act = a.actions[o];
-  c.old = a.old_logp[o];
-  c.ref = a.ref_logp ? a.ref_logp[o] : 0.f;
-  c.adv = a.per_choice ? a.adv[o] : a.adv[s];
+  c.act = (a.actions + o)[k];
+  c.old = (a.old_logp + o)[k];
+  c.ref = a.ref_logp ? (a.ref_logp + o)[k] : 0.f;
+  c.adv = a.per_choice ? (a.adv + o)[k] : a.adv[s];
   return c;
 }
 // What the choices of one thread add to the loss's terms.
@@ -426,7 +416,7 @@ __device__ __forceinline__ float choice_slope(const PolicyLossArgs& a, const Cho
     q = q * k + 1.f / 24;
     q = q * k + 1.f / 6;
     q = (q * k + 0.5f) * k * k;
-    if (!(fabsf(k) < 1.f)) q = (exp_fast(k) - 1.f) - k;
+    if (__any(!(fabsf(k) < 1.f)) && !(fabsf(k) < 1.f)) q = (exp_fast(k) - 1.f) - k;
     t.kl += made ? q : 0.f;
     if (a.kl_coef != 0.f) slope -= a.kl_coef * (k + q);  // (not 0 times infinity)
   }
@@ -514,8 +504,12 @@ __device__ __forceinline__ void quad_store(void* grad, int bf16, long long row, 
 template <int G, int N>
 constexpr bool kDirect = G * N <= 32;
 
+// Workgroups that a CU holds at once by their registers (without spilling any).
+template <int G, int N>
+constexpr int kLossWaves = N > 4 ? 4 : G == 1 ? 5 : 6;
+
 template <int G, int N, bool TAIL>
-__global__ void __launch_bounds__(kPolicyThreads) policy_loss_rows_kernel(PolicyLossArgs a, int chunk) {
+__global__ void __launch_bounds__(kPolicyThreads, (kLossWaves<G, N>)) policy_loss_rows_kernel(PolicyLossArgs a, int chunk) {
   constexpr bool DIRECT = kDirect<G, N>;
   constexpr int T = kPolicyThreads / G;
   constexpr int PARTS = DIRECT ? G : 1;
@@ -527,9 +521,7 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_loss_rows_kernel(Policy
   if (threadIdx.x < kPolicyThreads / 64 * 4) (&terms[0][0])[threadIdx.x] = 0.;
   const long long tiles = (a.count + T - 1) / T;
 #pragma unroll 1
-  for (long long round = 0;; ++round) {
-    const long long tile = tile_of(round, tiles);
-    if (tile >= tiles) break;
+  for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     unsigned tid = threadIdx.x;
     int K = a.K;
     asm volatile("" : "+v"(tid));
@@ -542,12 +534,13 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_loss_rows_kernel(Policy
     float4* mine = reinterpret_cast<float4*>(lds + row * stride);
     const long long r0 = tile * T;
     const bool ok = r0 + row < a.count;
-    const int part = tid / T;
     const int mine_row = tid % T;  // whose choices this thread takes, G rollouts apart
-    long long at = part * a.count + r0 + mine_row;
+    int part = tid / T;
+    if constexpr (T % 64 == 0) part = __builtin_amdgcn_readfirstlane(part);
+    long long at = part * a.count + r0;
     auto fetch = [&](int s, long long o) {
       Choice c{-1, 0.f, 0.f, 0.f};
-      if (s < a.samples && r0 + mine_row < a.count) c = choice_read(a, s, o);
+      if (s < a.samples && r0 + mine_row < a.count) c = choice_read(a, s, o, mine_row);
       return c;
     };
     Choice next = fetch(part, at);
@@ -716,7 +709,7 @@ __global__ void __launch_bounds__(kLongThreads) policy_loss_long_kernel(PolicyLo
     bool near = false;
     Terms add;
     for (int s = lane; s < a.samples; s += kLongThreads) {
-      const Choice c = choice_read(a, s, (long long)s * a.count + r);
+      const Choice c = choice_read(a, s, (long long)s * a.count + r, 0u);
       const bool real = (unsigned)c.act < (unsigned)a.K;
       const Ratio ratio(a, c, real ? floor_d(row[c.act] - m) : __builtin_nanf(""), lz);
       const bool here = real && ratio.open(c, lz);
@@ -729,7 +722,7 @@ __global__ void __launch_bounds__(kLongThreads) policy_loss_long_kernel(PolicyLo
       const double zr = block_sum_d<kLongThreads>(sum_exp_d<kLongThreads>(row, a.K, lane, m), redd);
       for (int s = lane; s < a.samples; s += kLongThreads) {
         if (__float_as_int(pairs[s].x) != -2) continue;
-        const Choice c = choice_read(a, s, (long long)s * a.count + r);
+        const Choice c = choice_read(a, s, (long long)s * a.count + r, 0u);
         const float x = row[c.act];
         Ratio ratio(a, c, x - m, lz);
         ratio.over = over_d(a, c, x, m, zr);
@@ -869,7 +862,9 @@ hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) {
         const int rounds = (a.samples + S::G - 1) / S::G;
         const int chunk = std::max(1, std::min(rounds, fit)) * S::G;
         const size_t lds = kDirect<S::G, S::N> ? (size_t)table * (1 + S::G) : table + (size_t)chunk * T * 8;
-        grid = policy_grid<S::G>(a.count, kPolicyParts);
+        // as many workgroups as run at once: a second, smaller round of them would leave CUs idle
+        static_assert(kPolicyCus * kLossWaves<S::G, S::N> <= kPolicyParts, "partial sums");
+        grid = policy_grid<S::G>(a.count, kPolicyCus * std::min<long long>(kLossWaves<S::G, S::N>, 163840 / (lds + 4096)));
         hipLaunchKernelGGL((policy_loss_rows_kernel<S::G, S::N, S::TAIL>), grid, dim3(kPolicyThreads), lds, st, a, chunk);
       },
       [&] {
