@@ -1,5 +1,13 @@
 // The optimiser step over many tensors: the 2-norm of their gradients, AdamW
 // with float32 or 8-bit moments, and the values that 8-bit moments stand for.
+//
+// Streaming passes over chunks of kTensorChunk values, a workgroup each; the
+// tensors of a launch are a kernel argument, so that hundreds of small ones
+// take a few launches and a step can be recorded.  A wave takes runs of 256
+// values, four neighbours a lane, which is also a block of the 8-bit moments:
+// its largest exponents are found in the wave.  Nothing is read or written
+// twice: 28 bytes a value with float32 moments and gradients, 14 with 8-bit
+// moments and bf16 gradients.
 #pragma once
 
 #include "kernels.hpp"
@@ -7,9 +15,8 @@
 
 namespace lr {
 
-__device__ __forceinline__ float grad_at(const void* g, long long i, int bf16) {
-  return bf16 ? __uint_as_float((uint32_t) static_cast<const uint16_t*>(g)[i] << 16) : static_cast<const float*>(g)[i];
-}
+constexpr int kOptThreads = 256;
+constexpr int kOptRuns = kTensorChunk / kOptThreads / 4;  // of 256 values, a wave's in a chunk
 
 // Random bits: two rounds of multiply and shift (the odd integers next to
 // 2^32 / golden ratio and 2^32 (sqrt 2 - 1)).
@@ -22,33 +29,122 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
 // Tensor of the list that chunk c of the launch belongs to.
 __device__ __forceinline__ int tensor_of(const TensorList& l, long long c) {
   int lo = 0;
-  for (int i = 1; i < l.num; ++i) lo = c >= l.t[i].chunk0 ? i : lo;
+  int hi = l.num;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (c >= l.t[mid].chunk0) lo = mid;
+    else hi = mid;
+  }
   return lo;
 }
 
-__global__ void __launch_bounds__(256) grad_norm_kernel(TensorList l, int bf16, double* __restrict__ part) {
-  __shared__ double red[4];
-  double s = 0.;
-  for (long long c = blockIdx.x; c < l.chunks; c += gridDim.x) {
-    const TensorEntry& t = l.t[tensor_of(l, c)];
-    for (int j = threadIdx.x; j < kTensorChunk; j += 256) {
-      const long long i = (c - t.chunk0) * kTensorChunk + j;
-      const double g = i < t.count ? (double)grad_at(t.grad, i, bf16) : 0.;
-      s += g * g;
-    }
+// Values i .. i + 3 of a tensor, any alignment; FULL: all are there.
+template <bool FULL>
+__device__ __forceinline__ void quad_f32(const void* p, long long i, long long count, float (&v)[4]) {
+  const float* __restrict__ x = static_cast<const float*>(p);
+  if (FULL) {
+    const Quad q = *reinterpret_cast<const Quad*>(x + i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = q.v[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = i + j < count ? x[i + j] : 0.f;
   }
-  s = block_sum_d<256>(s, red);
-  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+template <bool FULL>
+__device__ __forceinline__ void quad_grad(const void* p, int bf16, long long i, long long count, float (&v)[4]) {
+  if (!bf16) return quad_f32<FULL>(p, i, count, v);
+  const uint16_t* __restrict__ x = static_cast<const uint16_t*>(p);
+  if (FULL) {
+    const QuadBf16 q = *reinterpret_cast<const QuadBf16*>(x + i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(j % 2 ? q.v[j / 2] & 0xFFFF0000u : q.v[j / 2] << 16);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = i + j < count ? __uint_as_float((uint32_t)x[i + j] << 16) : 0.f;
+  }
+}
+struct __attribute__((packed, aligned(1))) Bytes4 {
+  uint32_t w;
+};
+template <bool FULL>
+__device__ __forceinline__ uint32_t quad_codes(const void* p, long long i, long long count) {
+  const uint8_t* __restrict__ x = static_cast<const uint8_t*>(p);
+  if (FULL) return reinterpret_cast<const Bytes4*>(x + i)->w;
+  uint32_t w = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (i + j < count) w |= (uint32_t)x[i + j] << (8 * j);
+  return w;
+}
+template <bool FULL>
+__device__ __forceinline__ void put_f32(void* p, long long i, long long count, const float (&v)[4]) {
+  float* x = static_cast<float*>(p);
+  if (FULL) {
+    *reinterpret_cast<Quad*>(x + i) = Quad{{v[0], v[1], v[2], v[3]}};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i + j < count) x[i + j] = v[j];
+  }
+}
+template <bool FULL>
+__device__ __forceinline__ void put_codes(void* p, long long i, long long count, uint32_t w) {
+  uint8_t* x = static_cast<uint8_t*>(p);
+  if (FULL) {
+    *reinterpret_cast<Bytes4*>(x + i) = Bytes4{w};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i + j < count) x[i + j] = (uint8_t)(w >> (8 * j));
+  }
 }
 
-__global__ void __launch_bounds__(256) grad_norm_finish_kernel(const double* __restrict__ part, int n, float* norm) {
-  __shared__ double red[4];
+// ---- norm ------------------------------------------------------------------
+// Squares and sums in float64: no square of a float32 leaves its range.
+template <int THREADS>
+__device__ __forceinline__ double grad_square_sum(const TensorList& l, int bf16, long long chunk, long long step) {
   double s = 0.;
-  for (int b = threadIdx.x; b < n; b += 256) s += part[b];
-  s = block_sum_d<256>(s, red);
+  for (; chunk < l.chunks; chunk += step) {
+    const TensorEntry& t = l.t[tensor_of(l, chunk)];
+    const long long base = (chunk - t.chunk0) * kTensorChunk;
+    auto one = [&](auto full) {
+      constexpr int QUADS = kTensorChunk / THREADS / 4;
+      float v[QUADS][4];
+#pragma unroll
+      for (int q = 0; q < QUADS; ++q)
+        quad_grad<decltype(full)::value>(t.grad, bf16, base + 4 * (q * THREADS + (int)threadIdx.x), t.count, v[q]);
+#pragma unroll
+      for (int q = 0; q < QUADS; ++q)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s += (double)v[q][j] * (double)v[q][j];
+    };
+    if (t.count - base >= kTensorChunk) one(std::true_type{});
+    else one(std::false_type{});
+  }
+  return s;
+}
+__global__ void __launch_bounds__(kOptThreads) grad_norm_kernel(TensorList l, int bf16, double* __restrict__ part) {
+  __shared__ double red[kOptThreads / 64];
+  const double s = block_sum_d<kOptThreads>(grad_square_sum<kOptThreads>(l, bf16, blockIdx.x, gridDim.x), red);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+__global__ void __launch_bounds__(1024) grad_norm_finish_kernel(const double* __restrict__ part, int n, float* norm) {
+  __shared__ double red[16];
+  double s = 0.;
+  for (int b = threadIdx.x; b < n; b += 1024) s += part[b];
+  s = block_sum_d<1024>(s, red);
+  if (threadIdx.x == 0) *norm = (float)sqrt(s);
+}
+// A few chunks: one workgroup, one launch.
+constexpr int kNormOneChunks = 8;
+__global__ void __launch_bounds__(1024) grad_norm_one_kernel(TensorList l, int bf16, float* norm) {
+  __shared__ double red[16];
+  const double s = block_sum_d<1024>(grad_square_sum<1024>(l, bf16, 0, 1), red);
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
+// ---- AdamW -----------------------------------------------------------------
 // Products and sums that are rounded one by one (never fused): the moments are
 // defined by them.
 __device__ __forceinline__ float mul_rn(float a, float b) {
@@ -60,134 +156,226 @@ __device__ __forceinline__ float add_rn(float a, float b) {
   return a + b;
 }
 
-// 8-bit codes: value / (2 u), in [0, 1], of the seven or eight bits c.
-template <int LEAST>  // exponent of the smallest normal value
-__device__ __forceinline__ float code_value(uint32_t c) {
-  const uint32_t e = c >> 3;
-  const float f = (float)(c & 7u);
-  return e ? (8.f + f) * __uint_as_float((e + 126u + LEAST - 3u) << 23) : f * __uint_as_float((127u + LEAST - 3u) << 23);
+// 8-bit codes: with the code's seven or eight bits c in place (exponent and
+// three mantissa bits, as float32 has them), float32's own subnormal numbers
+// give the codes below the smallest normal value, 2^LEAST; two powers of two
+// then bring the exponent right.
+template <int LEAST>
+__device__ __forceinline__ float code_value(uint32_t c, float u) {
+  // (2^(127 + LEAST) times u: 2 u 2^LEAST over float32's 2^-126)
+  return __uint_as_float(c << 20) * __uint_as_float((254u + LEAST) << 23) * u;
 }
-// Code of the magnitude y in [0, 1) with 20 random bits.
+// Code of the magnitude y in [0, 1) with 20 random bits: below 2^LEAST, adding
+// 2^LEAST puts the codes' distances into the same bits as above it.
 template <int LEAST>
 __device__ __forceinline__ uint32_t code_of(float y, uint32_t bits) {
   const float least = __uint_as_float((127u + LEAST) << 23);
   const bool small = y < least;
   const uint32_t z = (__float_as_uint(small ? y + least : y) + bits) >> 20;
-  return z - ((126u + LEAST) << 3) - (small ? 8u : 0u);
+  return z - (small ? ((126u + LEAST) << 3) + 8u : (126u + LEAST) << 3);
+}
+// Largest magnitude of the wave as bits (NaN and infinity the largest).
+__device__ __forceinline__ uint32_t wave_max_bits(uint32_t x) {
+  auto dpp = [&](auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(ctrl)::value, 0xF, 0xF, false);
+  };
+  x = max(x, dpp(std::integral_constant<int, 0xB1>{}));
+  x = max(x, dpp(std::integral_constant<int, 0x4E>{}));
+  x = max(x, dpp(std::integral_constant<int, 0x141>{}));
+  x = max(x, dpp(std::integral_constant<int, 0x140>{}));
+  auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = max((uint32_t)r[0], (uint32_t)r[1]);
+  r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return max((uint32_t)r[0], (uint32_t)r[1]);
 }
 
-// One block of LST values per workgroup.
-__global__ void __launch_bounds__(256) adamw_kernel(TensorList l, AdamwArgs a) {
-  __shared__ float redf[4];
+// m and v after the step, p moved by them.
+__device__ __forceinline__ void adamw_values(const AdamwArgs& a, float clip, const float (&g4)[4], float (&m)[4],
+                                             float (&v)[4], float (&p)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float g = mul_rn(g4[j], clip);  // (exact for clip = 1)
+    m[j] = add_rn(mul_rn(m[j], a.b1), mul_rn(g, a.c1));
+    v[j] = add_rn(mul_rn(v[j], a.b2), mul_rn(mul_rn(g, g), a.c2));
+    // (the root's instruction takes no subnormal numbers)
+    const bool tiny = v[j] < 0x1p-100f;
+    const float root = __builtin_amdgcn_sqrtf(tiny ? v[j] * 0x1p64f : v[j]) * (tiny ? 0x1p-32f : 1.f);
+    p[j] = p[j] * a.keep - a.rate * m[j] * __builtin_amdgcn_rcpf(root * a.root + a.eps);
+  }
+}
+
+template <bool BITS8, bool BF16, bool FULL>
+__device__ __forceinline__ void adamw_chunk(const TensorEntry& t, const AdamwArgs& a, long long base) {
+  constexpr int RUNS = kOptRuns;
+  constexpr int AT_ONCE = BITS8 ? RUNS : 2;  // runs in flight
+  const int wave = threadIdx.x / 64;
+  const int lane = threadIdx.x % 64;
   float clip = 1.f;
   if (a.norm) {
     const float n = *a.norm;
     if (!(fabsf(n) <= 3.402823466e38f)) return;
     if (n > a.max_norm) clip = a.max_norm / n;
   }
-  for (long long c = blockIdx.x; c < l.chunks; c += gridDim.x) {
-    const int ti = tensor_of(l, c);
-    const TensorEntry& t = l.t[ti];
-    for (int j = threadIdx.x; j < kTensorChunk; j += 256) {
-      const long long i = (c - t.chunk0) * kTensorChunk + j;
-      const bool in = i < t.count;
-      const long long blk = ((c - t.chunk0) * kTensorChunk + (j & ~255)) / 256;
-      const bool blk_in = blk * 256 < t.count;
-      float m = 0.f;
-      float v = 0.f;
-      float g = 0.f;
-      float p = 0.f;
-      if (in) {
-        g = grad_at(t.grad, i, a.bf16);
-        p = t.param[i];
-        if (a.bits8) {
-          const uint32_t cm = static_cast<const uint8_t*>(t.m)[i];
-          const uint32_t cv = static_cast<const uint8_t*>(t.v)[i];
-          m = mul_rn(2.f * code_value<-14>(cm & 127u), t.scales[2 * blk]);
-          if (cm & 128u) m = -m;
-          v = mul_rn(2.f * code_value<-30>(cv), t.scales[2 * blk + 1]);
-        } else {
-          m = static_cast<const float*>(t.m)[i];
-          v = static_cast<const float*>(t.v)[i];
-        }
-        if (a.norm) g = mul_rn(g, clip);
-        m = add_rn(mul_rn(m, a.b1), mul_rn(g, a.c1));
-        v = add_rn(mul_rn(v, a.b2), mul_rn(mul_rn(g, g), a.c2));
-        t.param[i] = p * a.keep - a.rate * m / (sqrtf(v) * a.root + a.eps);
-        if (!a.bits8) {
-          static_cast<float*>(t.m)[i] = m;
-          static_cast<float*>(t.v)[i] = v;
-        }
+#pragma unroll
+  for (int r0 = 0; r0 < RUNS; r0 += AT_ONCE) {
+    float p[AT_ONCE][4], g[AT_ONCE][4];
+    float m[BITS8 ? 1 : AT_ONCE][4], v[BITS8 ? 1 : AT_ONCE][4];
+    uint32_t cm[AT_ONCE], cv[AT_ONCE];
+    float2 u[AT_ONCE];
+    // (a block past the tensor's end has no scales)
+    auto block = [&](int r) { return base / kStateBlock + (r0 + r) * (kOptThreads / 64) + wave; };
+    auto at = [&](int r) { return base + ((r0 + r) * (kOptThreads / 64) + wave) * 256 + 4 * lane; };
+#pragma unroll
+    for (int r = 0; r < AT_ONCE; ++r) {
+      const long long i = at(r);
+      quad_f32<FULL>(t.param, i, t.count, p[r]);
+      quad_grad<FULL>(t.grad, BF16, i, t.count, g[r]);
+      if constexpr (BITS8) {
+        cm[r] = quad_codes<FULL>(t.m, i, t.count);
+        cv[r] = quad_codes<FULL>(t.v, i, t.count);
+        u[r] = make_float2(0.f, 0.f);
+        if (FULL || block(r) * kStateBlock < t.count)
+          u[r] = make_float2(t.scales[2 * block(r)], t.scales[2 * block(r) + 1]);
+      } else {
+        quad_f32<FULL>(t.m, i, t.count, m[r]);
+        quad_f32<FULL>(t.v, i, t.count, v[r]);
       }
-      if (a.bits8) {
-        // (exponents are exact in float32)
-        uint32_t em = (uint32_t)block_reduce<256>((float)((__float_as_uint(m) >> 23) & 255u), OpMax{}, redf);
-        uint32_t ev = (uint32_t)block_reduce<256>((float)((__float_as_uint(v) >> 23) & 255u), OpMax{}, redf);
-        em = em < 27u ? 27u : em;
-        ev = ev < 27u ? 27u : ev;
-        if (in) {
-          const uint32_t key = mix32(t.key + (uint32_t)((unsigned long long)i >> 32));
-          const uint32_t h = mix32((uint32_t)i + key);
-          uint32_t cm = 0;
-          uint32_t cv = 0;
-          if (em < 253u) {
-            cm = code_of<-14>(fabsf(m) * __uint_as_float((253u - em) << 23), h & 0xFFFFFu);
-            if (m < 0.f) cm |= 128u;
-          }
-          if (ev < 253u) {
-            cv = code_of<-30>(v * __uint_as_float((253u - ev) << 23), h >> 12);
-            if (v > 0.f && cv == 0u) cv = 1u;
-          }
-          static_cast<uint8_t*>(t.m)[i] = (uint8_t)cm;
-          static_cast<uint8_t*>(t.v)[i] = (uint8_t)cv;
+    }
+#pragma unroll
+    for (int r = 0; r < AT_ONCE; ++r) {
+      const long long i = at(r);
+      if constexpr (!BITS8) {
+        adamw_values(a, clip, g[r], m[r], v[r], p[r]);
+        put_f32<FULL>(t.param, i, t.count, p[r]);
+        put_f32<FULL>(t.m, i, t.count, m[r]);
+        put_f32<FULL>(t.v, i, t.count, v[r]);
+      } else {
+        float mm[4], vv[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t c = cm[r] >> (8 * j);
+          const float x = code_value<-14>(c & 127u, u[r].x);
+          mm[j] = __uint_as_float(__float_as_uint(x) ^ ((c & 128u) << 24));
+          vv[j] = code_value<-30>((cv[r] >> (8 * j)) & 255u, u[r].y);
         }
-        if (threadIdx.x == 0 && blk_in) {
-          t.scales[2 * blk] = em < 253u ? __uint_as_float(em << 23) : __builtin_nanf("");
-          t.scales[2 * blk + 1] = ev < 253u ? __uint_as_float(ev << 23) : __builtin_nanf("");
+        adamw_values(a, clip, g[r], mm, vv, p[r]);
+        put_f32<FULL>(t.param, i, t.count, p[r]);
+        uint32_t top_m = 0, top_v = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          top_m = max(top_m, __float_as_uint(fabsf(mm[j])));
+          top_v = max(top_v, __float_as_uint(vv[j]) & 0x7FFFFFFFu);
+        }
+        // exponents of the block, held where a scale and its inverse are normal numbers
+        uint32_t em = wave_max_bits(top_m) >> 23;
+        uint32_t ev = wave_max_bits(top_v) >> 23;
+        em = max(em, 27u);
+        ev = max(ev, 27u);
+        const float down_m = __uint_as_float((253u - min(em, 253u)) << 23);
+        const float down_v = __uint_as_float((253u - min(ev, 253u)) << 23);
+        const uint32_t key = mix32(t.key + (uint32_t)((unsigned long long)i >> 32));
+        uint32_t wm = 0, wv = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t h = mix32((uint32_t)i + j + key);
+          uint32_t c = code_of<-14>(fabsf(mm[j]) * down_m, h & 0xFFFFFu);
+          c = c & 127u;
+          if (mm[j] < 0.f) c |= 128u;
+          wm |= c << (8 * j);
+          c = code_of<-30>(vv[j] * down_v, h >> 12) & 255u;
+          c = vv[j] > 0.f && c == 0u ? 1u : c;
+          wv |= c << (8 * j);
+        }
+        if (em >= 253u) wm = 0;
+        if (ev >= 253u) wv = 0;
+        put_codes<FULL>(t.m, i, t.count, wm);
+        put_codes<FULL>(t.v, i, t.count, wv);
+        if (lane == 0 && (FULL || block(r) * kStateBlock < t.count)) {
+          t.scales[2 * block(r)] = em < 253u ? __uint_as_float(em << 23) : __builtin_nanf("");
+          t.scales[2 * block(r) + 1] = ev < 253u ? __uint_as_float(ev << 23) : __builtin_nanf("");
         }
       }
     }
   }
 }
 
-__global__ void __launch_bounds__(256) moments_kernel(TensorList l) {
+template <bool BITS8, bool BF16>
+__global__ void __launch_bounds__(kOptThreads) adamw_kernel(TensorList l, AdamwArgs a) {
   for (long long c = blockIdx.x; c < l.chunks; c += gridDim.x) {
     const TensorEntry& t = l.t[tensor_of(l, c)];
-    for (int j = threadIdx.x; j < kTensorChunk; j += 256) {
-      const long long i = (c - t.chunk0) * kTensorChunk + j;
-      if (i >= t.count) continue;
-      const uint32_t cm = static_cast<const uint8_t*>(t.m)[i];
-      const uint32_t cv = static_cast<const uint8_t*>(t.v)[i];
-      const float m = 2.f * code_value<-14>(cm & 127u) * t.scales[2 * (i / 256)];
-      t.param[i] = cm & 128u ? -m : m;
-      const_cast<float*>(static_cast<const float*>(t.grad))[i] = 2.f * code_value<-30>(cv) * t.scales[2 * (i / 256) + 1];
-    }
+    const long long base = (c - t.chunk0) * kTensorChunk;
+    if (t.count - base >= kTensorChunk) adamw_chunk<BITS8, BF16, true>(t, a, base);
+    else adamw_chunk<BITS8, BF16, false>(t, a, base);
   }
 }
 
+template <bool FULL>
+__device__ __forceinline__ void moments_chunk(const TensorEntry& t, long long base) {
+#pragma unroll
+  for (int r = 0; r < kOptRuns; ++r) {
+    const long long run = base + (r * (kOptThreads / 64) + threadIdx.x / 64) * 256;
+    const long long i = run + 4 * (threadIdx.x % 64);
+    if (!FULL && run >= t.count) break;
+    const uint32_t cm = quad_codes<FULL>(t.m, i, t.count);
+    const uint32_t cv = quad_codes<FULL>(t.v, i, t.count);
+    const float um = t.scales[2 * (run / kStateBlock)];
+    const float uv = t.scales[2 * (run / kStateBlock) + 1];
+    float m[4], v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t c = cm >> (8 * j);
+      m[j] = __uint_as_float(__float_as_uint(code_value<-14>(c & 127u, um)) ^ ((c & 128u) << 24));
+      v[j] = code_value<-30>((cv >> (8 * j)) & 255u, uv);
+    }
+    put_f32<FULL>(t.param, i, t.count, m);
+    put_f32<FULL>(const_cast<void*>(t.grad), i, t.count, v);
+  }
+}
+__global__ void __launch_bounds__(kOptThreads) moments_kernel(TensorList l) {
+  for (long long c = blockIdx.x; c < l.chunks; c += gridDim.x) {
+    const TensorEntry& t = l.t[tensor_of(l, c)];
+    const long long base = (c - t.chunk0) * kTensorChunk;
+    if (t.count - base >= kTensorChunk) moments_chunk<true>(t, base);
+    else moments_chunk<false>(t, base);
+  }
+}
+
+// ---- launches ----------------------------------------------------------------
 hipError_t launch_grad_norm(const TensorList* lists, int num, int bf16, double* part, float* norm, hipStream_t st) {
+  if (num == 1 && lists[0].chunks <= kNormOneChunks) {
+    hipLaunchKernelGGL(grad_norm_one_kernel, dim3(1), dim3(1024), 0, st, lists[0], bf16, norm);
+    return hipGetLastError();
+  }
   int parts = 0;
   for (int i = 0; i < num; ++i) {
-    if (lists[i].chunks <= 0) continue;
     const int grid = (int)std::min<long long>(lists[i].chunks, kNormParts);
-    hipLaunchKernelGGL(grad_norm_kernel, dim3(grid), dim3(256), 0, st, lists[i], bf16, part + parts);
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(grid), dim3(kOptThreads), 0, st, lists[i], bf16, part + parts);
     parts += grid;
   }
-  hipLaunchKernelGGL(grad_norm_finish_kernel, dim3(1), dim3(256), 0, st, part, parts, norm);
-  return hipGetLastError();
-}
-
-hipError_t launch_adamw(const TensorList& l, const AdamwArgs& a, hipStream_t st) {
-  if (l.chunks <= 0) return hipSuccess;
-  hipLaunchKernelGGL(adamw_kernel, dim3((unsigned)std::min<long long>(l.chunks, 1 << 16)), dim3(256), 0, st, l, a);
+  hipLaunchKernelGGL(grad_norm_finish_kernel, dim3(1), dim3(1024), 0, st, part, parts, norm);
   return hipGetLastError();
 }
 
 uint32_t tensor_key(uint32_t seed, uint32_t i) { return mix32(seed + 0x9E3779B9u * i); }
 
+static dim3 chunk_grid(const TensorList& l) { return dim3((unsigned)std::min<long long>(l.chunks, 1 << 22)); }
+
+hipError_t launch_adamw(const TensorList& l, const AdamwArgs& a, hipStream_t st) {
+  if (l.chunks <= 0) return hipSuccess;
+  auto go = [&](auto bits8, auto bf16) {
+    hipLaunchKernelGGL((adamw_kernel<decltype(bits8)::value, decltype(bf16)::value>), chunk_grid(l), dim3(kOptThreads),
+                       0, st, l, a);
+  };
+  if (a.bits8 && a.bf16) go(std::true_type{}, std::true_type{});
+  else if (a.bits8) go(std::true_type{}, std::false_type{});
+  else if (a.bf16) go(std::false_type{}, std::true_type{});
+  else go(std::false_type{}, std::false_type{});
+  return hipGetLastError();
+}
+
 hipError_t launch_moments(const TensorList& l, hipStream_t st) {
   if (l.chunks <= 0) return hipSuccess;
-  hipLaunchKernelGGL(moments_kernel, dim3((unsigned)std::min<long long>(l.chunks, 1 << 16)), dim3(256), 0, st, l);
+  hipLaunchKernelGGL(moments_kernel, chunk_grid(l), dim3(kOptThreads), 0, st, l);
   return hipGetLastError();
 }
 

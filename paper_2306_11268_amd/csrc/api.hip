@@ -626,6 +626,7 @@ std::vector<lr::TensorList> tensor_lists(const lr_param* params, int32_t num, ui
   return lists;
 }
 
+static_assert(LR_STATE_BLOCK == lr::kStateBlock, "block of the 8-bit moments");
 size_t scale_bytes(int64_t count) { return static_cast<size_t>((count + LR_STATE_BLOCK - 1) / LR_STATE_BLOCK) * 8; }
 
 // No C++ exception (out of host memory) leaves an entry point.

@@ -276,7 +276,8 @@ hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st);
 
 // The tensors of one launch of an optimiser step, worked in chunks of
 // kTensorChunk values (a kernel argument: a launch may be captured).
-constexpr int kTensorChunk = 2048;
+constexpr int kTensorChunk = 4096;
+constexpr int kStateBlock = 256;  // values that share the scales of 8-bit moments
 constexpr int kTensorsPerLaunch = 48;
 struct TensorEntry {
   float* param;
