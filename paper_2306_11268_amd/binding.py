@@ -537,10 +537,11 @@ def multichannel_train_step(nets, amps, phis, saveds, labels, kind: int = LR_LOS
 def _run_on(device, fn, *args) -> int:
     """fn(*args, stream) with the device current and on its current stream."""
     torch = _torch()
-    if torch.cuda.current_device() == device.index:
-        return fn(*args, _stream(device))
-    with torch.cuda.device(device):
-        return fn(*args, _stream(device))
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return fn(*args, _stream(device))
+    # (the stream's handle without the Python object around it, which takes 2 us)
+    return fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
 
 
 def _at(device, t, dtype, shape, name) -> Optional[int]:
@@ -623,21 +624,22 @@ def lr_policy_loss(logits, actions, old_logp, advantages, ref_logp=None, clip_lo
         raise ValueError(f"grad_dtype must be float32 or bfloat16, got {grad_dtype}")
     if want_grad and out_grad is None:
         out_grad = torch.empty(logits.shape, dtype=grad_dtype, device=dev)
-    both = torch.empty(5, dtype=torch.float32, device=dev) if want_loss else None
+    loss = torch.empty((), dtype=torch.float32, device=dev) if want_loss else None
+    terms = torch.empty(4, dtype=torch.float32, device=dev) if want_loss else None
     work = torch.empty(int(load().lr_policy_workspace_size()), dtype=torch.uint8, device=dev)
     policy = LrPolicy(clip_low, clip_high, kl_coef, entropy_coef, 1.0 / max(1, s * count) if scale is None else scale)
-    at = both.data_ptr() if want_loss else None
     _check(_run_on(dev, load().lr_policy_loss, ctypes.byref(policy),
                    _at(dev, logits, torch.float32, logits.shape, "logits"),
                    _at(dev, actions, torch.int32, shape, "actions"),
                    _at(dev, old_logp, torch.float32, shape, "old_logp"),
                    _at(dev, ref_logp, torch.float32, shape, "ref_logp"),
                    _at(dev, advantages, torch.float32, shape if per_choice else (s,), "advantages"),
-                   1 if per_choice else 0, s, count, k, at, at + 4 if want_loss else None,
+                   1 if per_choice else 0, s, count, k, loss.data_ptr() if want_loss else None,
+                   terms.data_ptr() if want_loss else None,
                    LR_GRAD_BF16 if grad_dtype == torch.bfloat16 else LR_GRAD_F32,
                    _at(dev, out_grad, grad_dtype, logits.shape, "grad_logits"), work.data_ptr(), work.numel()),
            "lr_policy_loss")
-    return (both[0], both[1:], out_grad) if want_loss else (None, None, out_grad)
+    return loss, terms, out_grad
 
 
 class TrainTensors:

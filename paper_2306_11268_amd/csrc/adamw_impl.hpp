@@ -1,7 +1,7 @@
 // The optimiser step over many tensors: the 2-norm of their gradients, AdamW
 // with float32 or 8-bit moments, and the values that 8-bit moments stand for.
 //
-// Streaming passes over chunks of kTensorChunk values, a workgroup each; the
+// Streaming passes over chunks of values, a workgroup each; the
 // tensors of a launch are a kernel argument, so that hundreds of small ones
 // take a few launches and a step can be recorded.  A wave takes runs of 256
 // values, four neighbours a lane, which is also a block of the 8-bit moments:
@@ -16,7 +16,7 @@
 namespace lr {
 
 constexpr int kOptThreads = 256;
-constexpr int kOptRuns = kTensorChunk / kOptThreads / 4;  // of 256 values, a wave's in a chunk
+constexpr int kOptRuns = kStepChunk / kOptThreads / 4;  // of 256 values, a wave's in a chunk
 
 // Random bits: two rounds of multiply and shift (the odd integers next to
 // 2^32 / golden ratio and 2^32 (sqrt 2 - 1)).
@@ -107,9 +107,9 @@ __device__ __forceinline__ double grad_square_sum(const TensorList& l, int bf16,
   double s = 0.;
   for (; chunk < l.chunks; chunk += step) {
     const TensorEntry& t = l.t[tensor_of(l, chunk)];
-    const long long base = (chunk - t.chunk0) * kTensorChunk;
+    const long long base = (chunk - t.chunk0) * kNormChunk;
     auto one = [&](auto full) {
-      constexpr int QUADS = kTensorChunk / THREADS / 4;
+      constexpr int QUADS = kNormChunk / THREADS / 4;
       float v[QUADS][4];
 #pragma unroll
       for (int q = 0; q < QUADS; ++q)
@@ -119,7 +119,7 @@ __device__ __forceinline__ double grad_square_sum(const TensorList& l, int bf16,
 #pragma unroll
         for (int j = 0; j < 4; ++j) s += (double)v[q][j] * (double)v[q][j];
     };
-    if (t.count - base >= kTensorChunk) one(std::true_type{});
+    if (t.count - base >= kNormChunk) one(std::true_type{});
     else one(std::false_type{});
   }
   return s;
@@ -137,10 +137,11 @@ __global__ void __launch_bounds__(1024) grad_norm_finish_kernel(const double* __
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 // A few chunks: one workgroup, one launch.
-constexpr int kNormOneChunks = 8;
-__global__ void __launch_bounds__(1024) grad_norm_one_kernel(TensorList l, int bf16, float* norm) {
-  __shared__ double red[16];
-  const double s = block_sum_d<1024>(grad_square_sum<1024>(l, bf16, 0, 1), red);
+constexpr int kNormOneValues = 32768;
+constexpr int kNormOneThreads = kNormChunk / 4;
+__global__ void __launch_bounds__(kNormOneThreads) grad_norm_one_kernel(TensorList l, int bf16, float* norm) {
+  __shared__ double red[kNormOneThreads / 64];
+  const double s = block_sum_d<kNormOneThreads>(grad_square_sum<kNormOneThreads>(l, bf16, 0, 1), red);
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
@@ -207,7 +208,7 @@ __device__ __forceinline__ void adamw_values(const AdamwArgs& a, float clip, con
 template <bool BITS8, bool BF16, bool FULL>
 __device__ __forceinline__ void adamw_chunk(const TensorEntry& t, const AdamwArgs& a, long long base) {
   constexpr int RUNS = kOptRuns;
-  constexpr int AT_ONCE = BITS8 ? RUNS : 2;  // runs in flight
+  constexpr int AT_ONCE = BITS8 || RUNS < 2 ? RUNS : 2;  // runs in flight
   const int wave = threadIdx.x / 64;
   const int lane = threadIdx.x % 64;
   float clip = 1.f;
@@ -303,8 +304,8 @@ template <bool BITS8, bool BF16>
 __global__ void __launch_bounds__(kOptThreads) adamw_kernel(TensorList l, AdamwArgs a) {
   for (long long c = blockIdx.x; c < l.chunks; c += gridDim.x) {
     const TensorEntry& t = l.t[tensor_of(l, c)];
-    const long long base = (c - t.chunk0) * kTensorChunk;
-    if (t.count - base >= kTensorChunk) adamw_chunk<BITS8, BF16, true>(t, a, base);
+    const long long base = (c - t.chunk0) * kStepChunk;
+    if (t.count - base >= kStepChunk) adamw_chunk<BITS8, BF16, true>(t, a, base);
     else adamw_chunk<BITS8, BF16, false>(t, a, base);
   }
 }
@@ -334,16 +335,16 @@ __device__ __forceinline__ void moments_chunk(const TensorEntry& t, long long ba
 __global__ void __launch_bounds__(kOptThreads) moments_kernel(TensorList l) {
   for (long long c = blockIdx.x; c < l.chunks; c += gridDim.x) {
     const TensorEntry& t = l.t[tensor_of(l, c)];
-    const long long base = (c - t.chunk0) * kTensorChunk;
-    if (t.count - base >= kTensorChunk) moments_chunk<true>(t, base);
+    const long long base = (c - t.chunk0) * kStepChunk;
+    if (t.count - base >= kStepChunk) moments_chunk<true>(t, base);
     else moments_chunk<false>(t, base);
   }
 }
 
 // ---- launches ----------------------------------------------------------------
 hipError_t launch_grad_norm(const TensorList* lists, int num, int bf16, double* part, float* norm, hipStream_t st) {
-  if (num == 1 && lists[0].chunks <= kNormOneChunks) {
-    hipLaunchKernelGGL(grad_norm_one_kernel, dim3(1), dim3(1024), 0, st, lists[0], bf16, norm);
+  if (num == 1 && lists[0].chunks <= kNormOneValues / kNormChunk) {
+    hipLaunchKernelGGL(grad_norm_one_kernel, dim3(1), dim3(kNormOneThreads), 0, st, lists[0], bf16, norm);
     return hipGetLastError();
   }
   int parts = 0;

@@ -605,7 +605,7 @@ int params_check(const lr_param* params, int32_t num) {
 
 // The tensors in lists of one launch each, empty ones left out; the random
 // bits' keys count every tensor.
-std::vector<lr::TensorList> tensor_lists(const lr_param* params, int32_t num, uint32_t seed) {
+std::vector<lr::TensorList> tensor_lists(const lr_param* params, int32_t num, uint32_t seed, int chunk) {
   std::vector<lr::TensorList> lists;
   for (int32_t i = 0; i < num; ++i) {
     const lr_param& p = params[i];
@@ -621,7 +621,7 @@ std::vector<lr::TensorList> tensor_lists(const lr_param* params, int32_t num, ui
     t.count = static_cast<long long>(p.count);
     t.chunk0 = l.chunks;
     t.key = lr::tensor_key(seed, static_cast<uint32_t>(i));
-    l.chunks += (t.count + lr::kTensorChunk - 1) / lr::kTensorChunk;
+    l.chunks += (t.count + chunk - 1) / chunk;
   }
   return lists;
 }
@@ -1421,7 +1421,7 @@ int lr_grad_norm(const lr_param* params, int32_t num, int32_t grad_type, float* 
   }
   return no_throw([&] {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const std::vector<lr::TensorList> lists = tensor_lists(params, num, 0);
+    const std::vector<lr::TensorList> lists = tensor_lists(params, num, 0, lr::kNormChunk);
     return run_timed("grad_norm", st, [&] {
       return lr::launch_grad_norm(lists.data(), static_cast<int>(lists.size()), grad_type == LR_GRAD_BF16 ? 1 : 0,
                                   static_cast<double*>(d_work), d_norm, st);
@@ -1475,7 +1475,7 @@ int lr_adamw_update(const lr_param* params, int32_t num, int32_t grad_type, int3
     a.bf16 = grad_type == LR_GRAD_BF16 ? 1 : 0;
     a.bits8 = bits8 ? 1 : 0;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const std::vector<lr::TensorList> lists = tensor_lists(params, num, seed);
+    const std::vector<lr::TensorList> lists = tensor_lists(params, num, seed, lr::kStepChunk);
     return run_timed(bits8 ? "adamw8" : "adamw", st, [&] {
       for (const lr::TensorList& l : lists) {
         const hipError_t e = lr::launch_adamw(l, a, st);
@@ -1508,7 +1508,7 @@ int lr_adamw_moments(const lr_param* params, int32_t num, float* const* d_m_out,
     }
     if (ranges_alias(ranges)) return LR_E_ALIAS;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const std::vector<lr::TensorList> lists = tensor_lists(outs.data(), num, 0);
+    const std::vector<lr::TensorList> lists = tensor_lists(outs.data(), num, 0, lr::kStepChunk);
     return run_timed("adamw_moments", st, [&] {
       for (const lr::TensorList& l : lists) {
         const hipError_t e = lr::launch_moments(l, st);

@@ -274,11 +274,12 @@ struct PolicyLossArgs {
 };
 hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st);
 
-// The tensors of one launch of an optimiser step, worked in chunks of
-// kTensorChunk values (a kernel argument: a launch may be captured).
-constexpr int kTensorChunk = 4096;
+// The tensors of one launch of an optimiser step, worked in chunks of so many
+// values (a kernel argument: a launch may be captured).
+constexpr int kNormChunk = 4096;
+constexpr int kStepChunk = 1024;  // of lr_adamw_update and lr_adamw_moments
 constexpr int kStateBlock = 256;  // values that share the scales of 8-bit moments
-constexpr int kTensorsPerLaunch = 48;
+constexpr int kTensorsPerLaunch = 60;
 struct TensorEntry {
   float* param;
   const void* grad;
@@ -307,6 +308,7 @@ struct AdamwArgs {
   int bf16;
   int bits8;
 };
+static_assert(sizeof(TensorList) + sizeof(AdamwArgs) + 64 <= 4096, "kernel arguments");
 hipError_t launch_adamw(const TensorList& l, const AdamwArgs& a, hipStream_t st);
 // m and v of 8-bit moments as float32 (into param and grad of the entries).
 hipError_t launch_moments(const TensorList& l, hipStream_t st);

@@ -88,7 +88,10 @@ def table(*params):
 def test_grad_norm():
     lib = lb.load()
     w = lib.lr_grad_norm_workspace_size(2)
-    assert w == 2048 * 8 and lib.lr_grad_norm_workspace_size(0) == w and lib.lr_grad_norm_workspace_size(49) == 2 * w
+    assert w > 0 and lib.lr_grad_norm_workspace_size(0) == w
+    # one set of partial sums for each launch, of a few dozen tensors
+    sizes = [lib.lr_grad_norm_workspace_size(n) for n in range(1, 500)]
+    assert all(b >= a and b % w == 0 for a, b in zip(sizes, sizes[1:])) and sizes[-1] <= 16 * w
     assert lib.lr_grad_norm_workspace_size(-1) == -SIZE and lib.lr_grad_norm_workspace_size(65537) == -SIZE
     f = lambda t, num, gt=0, norm=A[0], work=A[1], size=w: lib.lr_grad_norm(t, num, gt, norm, work, size, None)  # noqa: E731
     t = table(param(0), param(1))
