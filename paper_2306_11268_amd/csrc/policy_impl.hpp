@@ -244,6 +244,8 @@ __device__ __forceinline__ void running_join(Running& w, float* red) {
 constexpr int kLongThreads = 512;
 constexpr int kLongPer = 16;                           // values a thread has in flight
 constexpr int kLongStep = kLongThreads * kLongPer;     // values of a round
+constexpr int kLongWaves = 4;                          // of a SIMD
+constexpr int kMaxRollouts = 1024;                     // of a call
 constexpr int kLongSamples = 4;                        // rollouts that one pass over the logits serves
 
 __global__ void __launch_bounds__(kLongThreads) policy_draw_long_kernel(PolicyDrawArgs a) {
@@ -686,19 +688,33 @@ __global__ void __launch_bounds__(kPolicyThreads, (kLossWaves<G, N>)) policy_los
 // to a CU, whose loads then wait for its own arithmetic.  The gradient is
 // written as if no level had been chosen; then the first rollout that chose a
 // level adds the slopes of all that did, in their order, and writes that value
-// again.
-__global__ void __launch_bounds__(kLongThreads) policy_loss_long_kernel(PolicyLossArgs a) {
+// again.  A thread's first choice and its logit are read before the row.
+__global__ void __launch_bounds__(kLongThreads, kLongWaves) policy_loss_long_kernel(PolicyLossArgs a) {
   __shared__ float red[kLongThreads / 64];
   __shared__ double redd[kLongThreads / 64];
-  __shared__ float2 pairs[1024];  // (as many rollouts as a call may have)
-  const int lane = threadIdx.x;
-  double t[4] = {0., 0., 0., 0.};
+  __shared__ float2 pairs[kMaxRollouts];
+  __shared__ double terms[kLongThreads / 64][4];  // of each wave
+  if (threadIdx.x < kLongThreads / 64 * 4) (&terms[0][0])[threadIdx.x] = 0.;
+#pragma unroll 1
   for (long long r = blockIdx.x; r < a.count; r += gridDim.x) {
-    const float* __restrict__ row = a.logits + r * a.K;
+    int tid = threadIdx.x;
+    int K = a.K;
+    asm volatile("" : "+v"(tid));
+    asm volatile("" : "+s"(K));
+    const float* __restrict__ row = a.logits + r * K;
+    auto fetch = [&](int s, float& x) {
+      const Choice c = choice_read(a, s, (long long)s * a.count + r, 0u);
+      x = (unsigned)c.act < (unsigned)K ? row[c.act] : 0.f;
+      return c;
+    };
+    Choice c0{-1, 0.f, 0.f, 0.f};
+    float x0 = 0.f;
+    if (tid < a.samples) c0 = fetch(tid, x0);
     Running run;
-    for (int k0 = 0; k0 < a.K; k0 += kLongStep) {
+#pragma unroll 1
+    for (int k0 = 0; k0 < K; k0 += kLongStep) {
       float x[kLongPer];
-      row_read<kLongThreads, true>(row + k0, a.K - k0, lane, -INFINITY, x);
+      row_read<kLongThreads, true>(row + k0, K - k0, tid, -INFINITY, x);
       run.add(x);
     }
     running_join<kLongThreads>(run, red);
@@ -708,10 +724,13 @@ __global__ void __launch_bounds__(kLongThreads) policy_loss_long_kernel(PolicyLo
     const float h = lz - run.zd * inv_z;
     bool near = false;
     Terms add;
-    for (int s = lane; s < a.samples; s += kLongThreads) {
-      const Choice c = choice_read(a, s, (long long)s * a.count + r, 0u);
-      const bool real = (unsigned)c.act < (unsigned)a.K;
-      const Ratio ratio(a, c, real ? floor_d(row[c.act] - m) : __builtin_nanf(""), lz);
+#pragma unroll 1
+    for (int s = tid; s < a.samples; s += kLongThreads) {
+      Choice c = c0;
+      float x = x0;
+      if (s != tid) c = fetch(s, x);
+      const bool real = (unsigned)c.act < (unsigned)K;
+      const Ratio ratio(a, c, real ? floor_d(x - m) : __builtin_nanf(""), lz);
       const bool here = real && ratio.open(c, lz);
       near |= here;
       // (an undecided choice is left to the second pass)
@@ -719,36 +738,35 @@ __global__ void __launch_bounds__(kLongThreads) policy_loss_long_kernel(PolicyLo
       pairs[s] = make_float2(__int_as_float(here ? -2 : (c.act < 0 ? -1 : c.act)), g);
     }
     if (__syncthreads_or(near)) {
-      const double zr = block_sum_d<kLongThreads>(sum_exp_d<kLongThreads>(row, a.K, lane, m), redd);
-      for (int s = lane; s < a.samples; s += kLongThreads) {
+      const double zr = block_sum_d<kLongThreads>(sum_exp_d<kLongThreads>(row, K, tid, m), redd);
+#pragma unroll 1
+      for (int s = tid; s < a.samples; s += kLongThreads) {
         if (__float_as_int(pairs[s].x) != -2) continue;
-        const Choice c = choice_read(a, s, (long long)s * a.count + r, 0u);
-        const float x = row[c.act];
+        float x;
+        const Choice c = fetch(s, x);
         Ratio ratio(a, c, x - m, lz);
         ratio.over = over_d(a, c, x, m, zr);
-        const float g = choice_slope(a, c, ratio, h, add);
-        pairs[s] = make_float2(__int_as_float(c.act), g);
+        pairs[s] = make_float2(__int_as_float(c.act), choice_slope(a, c, ratio, h, add));
       }
       __syncthreads();
     }
-    t[0] -= (double)add.gain;
-    t[1] += (double)add.kl;
-    t[2] += (double)add.entropy;
-    t[3] += (double)add.cut;
+    terms_add(add, terms[tid / 64]);
     if (a.grad) {
+      // (every wave for itself)
       float slopes = 0.f;
       float made = 0.f;
-      for (int s = 0; s < a.samples; ++s) {
+      for (int s = tid % 64; s < a.samples; s += 64) {
         const float2 c = pairs[s];
-        if (__float_as_int(c.x) >= 0) {
-          made += 1.f;
-          slopes += c.y;
-        }
+        made += __float_as_int(c.x) >= 0 ? 1.f : 0.f;
+        slopes += __float_as_int(c.x) >= 0 ? c.y : 0.f;
       }
+      slopes = lanes_reduce<64>(slopes, OpSum{});
+      made = lanes_reduce<64>(made, OpSum{});
       const float w = a.scale * a.entropy_coef * made;
-      for (int k0 = 0; k0 < a.K; k0 += kLongStep) {
+#pragma unroll 1
+      for (int k0 = 0; k0 < K; k0 += kLongStep) {
         float x[kLongPer];
-        row_read<kLongThreads, true>(row + k0, a.K - k0, lane, -INFINITY, x);
+        row_read<kLongThreads, true>(row + k0, K - k0, tid, -INFINITY, x);
 #pragma unroll
         for (int i = 0; i < kLongPer; ++i) {
           const float d = x[i] - m;
@@ -756,12 +774,13 @@ __global__ void __launch_bounds__(kLongThreads) policy_loss_long_kernel(PolicyLo
         }
 #pragma unroll
         for (int i = 0; i < kLongPer; i += 4)
-          quad_store<true>(a.grad, a.bf16, r * a.K, a.K, k0 + quad_col<kLongThreads>(lane, i), &x[i]);
+          quad_store<true>(a.grad, a.bf16, r * K, K, k0 + quad_col<kLongThreads>(tid, i), &x[i]);
       }
       __syncthreads();  // (the row's stores come before those below)
-      for (int s = lane; s < a.samples; s += kLongThreads) {
+#pragma unroll 1
+      for (int s = tid; s < a.samples; s += kLongThreads) {
         const int act = __float_as_int(pairs[s].x);
-        if (act < 0 || act >= a.K) continue;
+        if (act < 0 || act >= K) continue;
         float g = 0.f;
         bool first = true;
         for (int o = 0; o < a.samples; ++o) {
@@ -771,15 +790,17 @@ __global__ void __launch_bounds__(kLongThreads) policy_loss_long_kernel(PolicyLo
           g += c.y;
         }
         if (!first) continue;
-        const float d = row[act] - m;
-        grad_store(a.grad, a.bf16, r * a.K + act, grad_value(g, exp_fast(d), floor_d(d), inv_z, lz, h, slopes, w));
+        const float d = (s == tid ? x0 : row[act]) - m;
+        grad_store(a.grad, a.bf16, r * K + act, grad_value(g, exp_fast(d), floor_d(d), inv_z, lz, h, slopes, w));
       }
     }
     __syncthreads();
   }
-  for (int i = 0; i < 4; ++i) {
-    const double s = block_sum_d<kLongThreads>(t[i], redd);
-    if (threadIdx.x == 0) a.part[4 * blockIdx.x + i] = s;
+  __syncthreads();
+  if (threadIdx.x < 4) {
+    double s = 0.;
+    for (int w = 0; w < kLongThreads / 64; ++w) s += terms[w][threadIdx.x];
+    a.part[4 * blockIdx.x + threadIdx.x] = s;
   }
 }
 
