@@ -14,7 +14,7 @@
 
 namespace lr {
 
-constexpr int kPolicyRowMax = 1024;
+constexpr int kPolicyRowMax = 2048;
 constexpr int kPolicyThreads = 256;
 constexpr int kPolicyCus = 256;  // of the MI355X
 
@@ -244,7 +244,6 @@ __device__ __forceinline__ void running_join(Running& w, float* red) {
 constexpr int kLongThreads = 512;
 constexpr int kLongPer = 16;                           // values a thread has in flight
 constexpr int kLongStep = kLongThreads * kLongPer;     // values of a round
-constexpr int kLongWaves = 4;                          // of a SIMD
 constexpr int kMaxRollouts = 1024;                     // of a call
 constexpr int kLongSamples = 4;                        // rollouts that one pass over the logits serves
 
@@ -490,8 +489,8 @@ __device__ __forceinline__ void quad_store(void* grad, int bf16, long long row, 
 // results do not change from run to run, also where rollouts chose the same
 // level).  3. The gradient from registers.
 //
-// DIRECT, rows of few levels: the thread that forms a slope adds it, into one of
-// the G tables that the threads of a row have; the gradient joins the tables.
+// PARTS > 0, rows of few levels: the thread that forms a slope adds it, into one
+// of the PARTS tables that the threads of a row have; the gradient joins them.
 // Otherwise the choices' levels and slopes go to shared memory, `chunk` rollouts
 // at a time, and a lane per row adds them in the logits' place.  (612500 rows of
 // 16 levels, 32 rollouts: 165 us through the list, whose one adding wave the
@@ -501,23 +500,19 @@ __device__ __forceinline__ void quad_store(void* grad, int bf16, long long row, 
 // on a CU: nothing is carried from tile to tile but the terms, and the thread's
 // number and K are made new for each, or the compiler holds 70 registers of
 // addresses and comparisons across the loop.  Dynamic shared memory (K rounded
-// up to four): DIRECT float [1 + G][T][K], the logits first; else float [T][K]
-// and float2 [chunk][T].
-template <int G, int N>
-constexpr bool kDirect = G * N <= 32;
+// up to four, and padded off the banks' number): float [1 + PARTS][T][K], the
+// logits first; without tables float2 [chunk][T] behind them.
+__host__ __device__ constexpr int loss_stride(int K) { return (K + 3) / 4 * 4 + ((K + 3) / 4 % 2 ? 0 : 4); }
 
-// Workgroups that a CU holds at once by their registers (without spilling any).
-template <int G, int N>
-constexpr int kLossWaves = N > 4 ? 4 : G == 1 ? 5 : 6;
-
-template <int G, int N, bool TAIL>
-__global__ void __launch_bounds__(kPolicyThreads, (kLossWaves<G, N>)) policy_loss_rows_kernel(PolicyLossArgs a, int chunk) {
-  constexpr bool DIRECT = kDirect<G, N>;
+template <int G, int N, int PARTS, int WAVES, bool TAIL>
+__global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel(PolicyLossArgs a, int chunk) {
+  constexpr bool DIRECT = PARTS > 0;
   constexpr int T = kPolicyThreads / G;
-  constexpr int PARTS = DIRECT ? G : 1;
+  constexpr int TABLES = DIRECT ? PARTS : 1;
+  constexpr int STEP = DIRECT ? PARTS : G;  // rollouts of a round: threads that take a row's choices
   extern __shared__ __align__(16) float lds[];
   __shared__ float2 stat[T];         // log of the sum of exponentials, entropy
-  __shared__ float2 sums[PARTS][T];  // of the row's slopes and choices
+  __shared__ float2 sums[TABLES][T];  // of the row's slopes and choices
   __shared__ float stat_m[T];
   __shared__ double terms[kPolicyThreads / 64][4];  // of each wave
   if (threadIdx.x < kPolicyThreads / 64 * 4) (&terms[0][0])[threadIdx.x] = 0.;
@@ -530,19 +525,19 @@ __global__ void __launch_bounds__(kPolicyThreads, (kLossWaves<G, N>)) policy_los
     asm volatile("" : "+s"(K));
     const int lane = tid % G;
     const int row = tid / G;
-    const int stride = (K + 3) / 4 * 4;
+    const int stride = loss_stride(K);
     const int table = T * stride;
     float2* pairs = reinterpret_cast<float2*>(lds + table);
     float4* mine = reinterpret_cast<float4*>(lds + row * stride);
     const long long r0 = tile * T;
     const bool ok = r0 + row < a.count;
-    const int mine_row = tid % T;  // whose choices this thread takes, G rollouts apart
+    const int mine_row = tid % T;  // whose choices this thread takes, STEP rollouts apart
     int part = tid / T;
     if constexpr (T % 64 == 0) part = __builtin_amdgcn_readfirstlane(part);
     long long at = part * a.count + r0;
     auto fetch = [&](int s, long long o) {
       Choice c{-1, 0.f, 0.f, 0.f};
-      if (s < a.samples && r0 + mine_row < a.count) c = choice_read(a, s, o, mine_row);
+      if (s < a.samples && part < STEP && r0 + mine_row < a.count) c = choice_read(a, s, o, mine_row);
       return c;
     };
     Choice next = fetch(part, at);
@@ -569,7 +564,7 @@ __global__ void __launch_bounds__(kPolicyThreads, (kLossWaves<G, N>)) policy_los
       mine[c / 4] = make_float4(d[i], d[i + 1], d[i + 2], d[i + 3]);
       if (DIRECT) {
 #pragma unroll
-        for (int p = 1; p <= PARTS; ++p) mine[p * (table / 4) + c / 4] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p = 1; p <= TABLES; ++p) mine[p * (table / 4) + c / 4] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
     }
     z = lanes_reduce<G>(z, OpSum{});
@@ -592,8 +587,8 @@ __global__ void __launch_bounds__(kPolicyThreads, (kLossWaves<G, N>)) policy_los
     // (a tail of the row's choices: no lane leaves before its wave)
     auto choose = [&](int s, bool near_lds) {
       const Choice c = next;
-      at += G * a.count;
-      next = fetch(s + G, at);
+      at += STEP * a.count;
+      next = fetch(s + STEP, at);
       const bool real = (unsigned)c.act < (unsigned)K;
       float dx;
       if (near_lds) dx = row_d[real ? c.act : 0];
@@ -617,15 +612,18 @@ __global__ void __launch_bounds__(kPolicyThreads, (kLossWaves<G, N>)) policy_los
       }
     };
     if constexpr (DIRECT) {
+      static_assert(T * PARTS % 64 == 0, "whole waves take choices");
+      if (part < PARTS) {
 #pragma unroll 1
-      for (int s = 0; s < a.samples; s += G) collect(choose(s + part, true));
-      sums[part][mine_row] = make_float2(slopes, made);
+        for (int s = 0; s < a.samples; s += STEP) collect(choose(s + part, true));
+        sums[part][mine_row] = make_float2(slopes, made);
+      }
     } else {
 #pragma unroll 1
       for (int s0 = 0; s0 < a.samples; s0 += chunk) {
         const int s1 = min(s0 + chunk, a.samples);
 #pragma unroll 1
-        for (int s = s0; s < s1; s += G) {
+        for (int s = s0; s < s1; s += STEP) {
           const float2 c = choose(s + part, s0 == 0);
           if (s + part < s1) pairs[(s + part - s0) * T + mine_row] = c;
         }
@@ -651,7 +649,7 @@ __global__ void __launch_bounds__(kPolicyThreads, (kLossWaves<G, N>)) policy_los
     if (a.grad) {
       float2 all = sums[0][row];
 #pragma unroll
-      for (int p = 1; p < PARTS; ++p) {
+      for (int p = 1; p < TABLES; ++p) {
         all.x += sums[p][row].x;
         all.y += sums[p][row].y;
       }
@@ -662,7 +660,7 @@ __global__ void __launch_bounds__(kPolicyThreads, (kLossWaves<G, N>)) policy_los
         if (c >= K) continue;
         float4 q = mine[(DIRECT ? table / 4 : 0) + c / 4];
 #pragma unroll
-        for (int p = 2; p <= PARTS; ++p) {
+        for (int p = 2; p <= TABLES; ++p) {
           const float4 o = mine[p * (table / 4) + c / 4];
           q = make_float4(q.x + o.x, q.y + o.y, q.z + o.z, q.w + o.w);
         }
@@ -683,18 +681,22 @@ __global__ void __launch_bounds__(kPolicyThreads, (kLossWaves<G, N>)) policy_los
   }
 }
 
-// A workgroup per row of more than kPolicyRowMax levels, which is read twice
-// (the second time from the caches): in registers it would leave one workgroup
-// to a CU, whose loads then wait for its own arithmetic.  The gradient is
-// written as if no level had been chosen; then the first rollout that chose a
-// level adds the slopes of all that did, in their order, and writes that value
-// again.  A thread's first choice and its logit are read before the row.
-__global__ void __launch_bounds__(kLongThreads, kLongWaves) policy_loss_long_kernel(PolicyLossArgs a) {
-  __shared__ float red[kLongThreads / 64];
-  __shared__ double redd[kLongThreads / 64];
+// A workgroup per row of more than kPolicyRowMax levels.  HELD rounds of the
+// row (16 values a thread each) stay in registers between the sums and the
+// gradient, as many as still leave two workgroups to a CU, so that one loads
+// while the other computes; what a longer row has beyond them is read again
+// from the caches.  The gradient is written as if no level had been chosen;
+// then the first rollout that chose a level adds the slopes of all that did, in
+// their order, and writes that value again.  A thread's first choice and its
+// logit are read before the row.
+template <int THREADS, int HELD, int WAVES>
+__global__ void __launch_bounds__(THREADS, WAVES) policy_loss_long_kernel(PolicyLossArgs a) {
+  constexpr int STEP = THREADS * kLongPer;
+  __shared__ float red[THREADS / 64];
+  __shared__ double redd[THREADS / 64];
   __shared__ float2 pairs[kMaxRollouts];
-  __shared__ double terms[kLongThreads / 64][4];  // of each wave
-  if (threadIdx.x < kLongThreads / 64 * 4) (&terms[0][0])[threadIdx.x] = 0.;
+  __shared__ double terms[THREADS / 64][4];  // of each wave
+  if (threadIdx.x < THREADS / 64 * 4) (&terms[0][0])[threadIdx.x] = 0.;
 #pragma unroll 1
   for (long long r = blockIdx.x; r < a.count; r += gridDim.x) {
     int tid = threadIdx.x;
@@ -711,13 +713,22 @@ __global__ void __launch_bounds__(kLongThreads, kLongWaves) policy_loss_long_ker
     float x0 = 0.f;
     if (tid < a.samples) c0 = fetch(tid, x0);
     Running run;
+    float held[HELD][kLongPer];
+#pragma unroll
+    for (int b = 0; b < HELD; ++b) {
+      if ((b + 1) * STEP <= K) row_read<THREADS, false>(row + b * STEP, STEP, tid, -INFINITY, held[b]);
+      else row_read<THREADS, true>(row + b * STEP, K - b * STEP, tid, -INFINITY, held[b]);
+    }
+#pragma unroll
+    for (int b = 0; b < HELD; ++b)
+      if (b * STEP < K) run.add(held[b]);
 #pragma unroll 1
-    for (int k0 = 0; k0 < K; k0 += kLongStep) {
+    for (int k0 = HELD * STEP; k0 < K; k0 += STEP) {
       float x[kLongPer];
-      row_read<kLongThreads, true>(row + k0, K - k0, tid, -INFINITY, x);
+      row_read<THREADS, true>(row + k0, K - k0, tid, -INFINITY, x);
       run.add(x);
     }
-    running_join<kLongThreads>(run, red);
+    running_join<THREADS>(run, red);
     const float m = run.m;
     const float inv_z = 1.f / run.z;
     const float lz = logf(run.z);
@@ -725,7 +736,7 @@ __global__ void __launch_bounds__(kLongThreads, kLongWaves) policy_loss_long_ker
     bool near = false;
     Terms add;
 #pragma unroll 1
-    for (int s = tid; s < a.samples; s += kLongThreads) {
+    for (int s = tid; s < a.samples; s += THREADS) {
       Choice c = c0;
       float x = x0;
       if (s != tid) c = fetch(s, x);
@@ -738,9 +749,9 @@ __global__ void __launch_bounds__(kLongThreads, kLongWaves) policy_loss_long_ker
       pairs[s] = make_float2(__int_as_float(here ? -2 : (c.act < 0 ? -1 : c.act)), g);
     }
     if (__syncthreads_or(near)) {
-      const double zr = block_sum_d<kLongThreads>(sum_exp_d<kLongThreads>(row, K, tid, m), redd);
+      const double zr = block_sum_d<THREADS>(sum_exp_d<THREADS>(row, K, tid, m), redd);
 #pragma unroll 1
-      for (int s = tid; s < a.samples; s += kLongThreads) {
+      for (int s = tid; s < a.samples; s += THREADS) {
         if (__float_as_int(pairs[s].x) != -2) continue;
         float x;
         const Choice c = fetch(s, x);
@@ -763,10 +774,7 @@ __global__ void __launch_bounds__(kLongThreads, kLongWaves) policy_loss_long_ker
       slopes = lanes_reduce<64>(slopes, OpSum{});
       made = lanes_reduce<64>(made, OpSum{});
       const float w = a.scale * a.entropy_coef * made;
-#pragma unroll 1
-      for (int k0 = 0; k0 < K; k0 += kLongStep) {
-        float x[kLongPer];
-        row_read<kLongThreads, true>(row + k0, K - k0, tid, -INFINITY, x);
+      auto write = [&](float (&x)[kLongPer], int k0) {
 #pragma unroll
         for (int i = 0; i < kLongPer; ++i) {
           const float d = x[i] - m;
@@ -774,11 +782,20 @@ __global__ void __launch_bounds__(kLongThreads, kLongWaves) policy_loss_long_ker
         }
 #pragma unroll
         for (int i = 0; i < kLongPer; i += 4)
-          quad_store<true>(a.grad, a.bf16, r * K, K, k0 + quad_col<kLongThreads>(tid, i), &x[i]);
+          quad_store<true>(a.grad, a.bf16, r * K, K, k0 + quad_col<THREADS>(tid, i), &x[i]);
+      };
+#pragma unroll
+      for (int b = 0; b < HELD; ++b)
+        if (b * STEP < K) write(held[b], b * STEP);
+#pragma unroll 1
+      for (int k0 = HELD * STEP; k0 < K; k0 += STEP) {
+        float x[kLongPer];
+        row_read<THREADS, true>(row + k0, K - k0, tid, -INFINITY, x);
+        write(x, k0);
       }
       __syncthreads();  // (the row's stores come before those below)
 #pragma unroll 1
-      for (int s = tid; s < a.samples; s += kLongThreads) {
+      for (int s = tid; s < a.samples; s += THREADS) {
         const int act = __float_as_int(pairs[s].x);
         if (act < 0 || act >= K) continue;
         float g = 0.f;
@@ -799,24 +816,31 @@ __global__ void __launch_bounds__(kLongThreads, kLongWaves) policy_loss_long_ker
   __syncthreads();
   if (threadIdx.x < 4) {
     double s = 0.;
-    for (int w = 0; w < kLongThreads / 64; ++w) s += terms[w][threadIdx.x];
+    for (int w = 0; w < THREADS / 64; ++w) s += terms[w][threadIdx.x];
     a.part[4 * blockIdx.x + threadIdx.x] = s;
   }
 }
 
-// The loss and its four terms from the workgroups' partial sums.
-__global__ void __launch_bounds__(256) policy_finish_kernel(const double* __restrict__ part, int n, float kl, float ent,
-                                                            float scale, float* loss, float* terms) {
-  __shared__ double red[4];
-  double t[4] = {0., 0., 0., 0.};
-  for (int b = threadIdx.x; b < n; b += 256)
-    for (int i = 0; i < 4; ++i) t[i] += part[4 * b + i];
-  for (int i = 0; i < 4; ++i) t[i] = block_sum_d<256>(t[i], red) * (double)scale;
-  if (threadIdx.x == 0) {
-    if (loss) *loss = (float)(t[0] + (kl != 0.f ? (double)kl * t[1] : 0.) - (double)ent * t[2]);
-    if (terms)
-      for (int i = 0; i < 4; ++i) terms[i] = (float)t[i];
-  }
+// The loss and its four terms from n workgroups' partial sums [n][4], a thread
+// for each and those of its kind a multiple of 1024 behind it.
+__global__ void __launch_bounds__(1024) policy_finish_kernel(const double* __restrict__ part, int n, float kl, float ent,
+                                                             float scale, float* loss, float* terms) {
+  __shared__ double red[16][4];
+  double s = 0.;
+  for (int e = threadIdx.x; e < 4 * n; e += 1024) s += part[e];
+#pragma unroll
+  for (int o = 32; o >= 4; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (threadIdx.x % 64 < 4) red[threadIdx.x / 64][threadIdx.x % 64] = s;
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  double t = 0.;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) t += red[w][threadIdx.x % 4];
+  t *= (double)scale;
+  if (threadIdx.x < 4 && terms) terms[threadIdx.x] = (float)t;
+  const double q = __shfl(t, 1, 64);
+  const double h = __shfl(t, 2, 64);
+  if (threadIdx.x == 0 && loss) *loss = (float)(t + (kl != 0.f ? (double)kl * q : 0.) - (double)ent * h);
 }
 
 // ---- launches ------------------------------------------------------------------
@@ -836,7 +860,28 @@ static void policy_rows_shape(int K, F&& rows) {
   else if (K <= 128) rows(Shape<8, 16, TAIL>{});
   else if (K <= 256) rows(Shape<16, 16, TAIL>{});
   else if (K <= 512) rows(Shape<32, 16, TAIL>{});
-  else rows(Shape<64, 16, TAIL>{});
+  else if (K <= 1024) rows(Shape<64, 16, TAIL>{});
+  else rows(Shape<64, 32, TAIL>{});
+}
+// The loss's rows: also how many threads of a row add slopes, and the
+// workgroups that a CU holds by their registers (without spilling any).
+template <int G_, int N_, int PARTS_, int WAVES_, bool TAIL_>
+struct LossShape {
+  static constexpr int G = G_, N = N_, PARTS = PARTS_, WAVES = WAVES_;
+  static constexpr bool TAIL = TAIL_;
+};
+template <bool TAIL, class F>
+static void loss_rows_shape(int K, F&& rows) {
+  if (K <= 4) rows(LossShape<1, 4, 1, 5, TAIL>{});
+  else if (K <= 8) rows(LossShape<1, 8, 1, 5, TAIL>{});
+  else if (K <= 16) rows(LossShape<2, 8, 2, 5, TAIL>{});
+  else if (K <= 32) rows(LossShape<4, 8, 2, 5, TAIL>{});
+  else if (K <= 64) rows(LossShape<8, 8, 2, 5, TAIL>{});
+  else if (K <= 128) rows(LossShape<8, 16, 0, 4, TAIL>{});
+  else if (K <= 256) rows(LossShape<16, 16, 0, 4, TAIL>{});
+  else if (K <= 512) rows(LossShape<32, 16, 0, 4, TAIL>{});
+  else if (K <= 1024) rows(LossShape<64, 16, 0, 4, TAIL>{});
+  else rows(LossShape<64, 32, 0, 3, TAIL>{});
 }
 template <class F, class L>
 static void policy_shape(int K, F&& rows, L&& longs) {
@@ -871,29 +916,42 @@ hipError_t launch_policy_draw(const PolicyDrawArgs& a, hipStream_t st) {
 hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) {
   if (a.count <= 0 || a.samples <= 0) return hipSuccess;
   dim3 grid;
-  policy_shape(
-      a.K,
-      [&](auto s) {
-        using S = decltype(s);
-        constexpr int T = kPolicyThreads / S::G;
-        const int table = T * ((a.K + 3) / 4 * 4) * 4;
-        // (the list: a whole number of the kernel's rounds of kPolicyThreads choices, in what leaves eight
-        // workgroups to a CU's 160 KB beside at most 16 KB of levels)
-        const int fit = (20480 - 192 - 20 * T - table) / (8 * kPolicyThreads);
-        const int rounds = (a.samples + S::G - 1) / S::G;
-        const int chunk = std::max(1, std::min(rounds, fit)) * S::G;
-        const size_t lds = kDirect<S::G, S::N> ? (size_t)table * (1 + S::G) : table + (size_t)chunk * T * 8;
-        // as many workgroups as run at once: a second, smaller round of them would leave CUs idle
-        static_assert(kPolicyCus * kLossWaves<S::G, S::N> <= kPolicyParts, "partial sums");
-        grid = policy_grid<S::G>(a.count, kPolicyCus * std::min<long long>(kLossWaves<S::G, S::N>, 163840 / (lds + 4096)));
-        hipLaunchKernelGGL((policy_loss_rows_kernel<S::G, S::N, S::TAIL>), grid, dim3(kPolicyThreads), lds, st, a, chunk);
-      },
-      [&] {
-        grid = dim3((unsigned)std::min<long long>(a.count, kPolicyParts));
-        hipLaunchKernelGGL(policy_loss_long_kernel, grid, dim3(kLongThreads), 0, st, a);
-      });
+  auto rows = [&](auto s) {
+    using S = decltype(s);
+    constexpr int T = kPolicyThreads / S::G;
+    const int table = T * loss_stride(a.K) * 4;
+    // (the list: a whole number of the kernel's rounds of kPolicyThreads choices, in what leaves as many
+    // workgroups to a CU's 160 KB as its registers do)
+    const int fixed = 192 + (12 + 8 * std::max(1, S::PARTS)) * T;
+    const int fit = (163840 / S::WAVES - fixed - table) / (8 * kPolicyThreads);
+    const int rounds = (a.samples + S::G - 1) / S::G;
+    const int chunk = std::max(1, std::min(rounds, std::min(fit, 8))) * S::G;
+    const size_t lds = S::PARTS ? (size_t)table * (1 + S::PARTS) : table + (size_t)chunk * T * 8;
+    // as many workgroups as run at once: a second, smaller round of them would leave CUs idle
+    static_assert(kPolicyCus * S::WAVES <= kPolicyParts, "partial sums");
+    grid = policy_grid<S::G>(a.count, kPolicyCus * std::min<long long>(S::WAVES, 163840 / (lds + fixed)));
+    hipLaunchKernelGGL((policy_loss_rows_kernel<S::G, S::N, S::PARTS, S::WAVES, S::TAIL>), grid, dim3(kPolicyThreads),
+                       lds, st, a, chunk);
+  };
+  if (a.K > kPolicyRowMax) {
+    grid = dim3((unsigned)std::min<long long>(a.count, kPolicyParts));
+    // (as many rounds held as the row has, up to four: 1500 rows of 65536 levels 210 -> 195 us from one to
+    // four, 6000 of 16384 179 -> 168 from one to two, but 205 with four, whose registers it does not fill)
+    if (a.K <= 256 * kLongPer)
+      hipLaunchKernelGGL((policy_loss_long_kernel<256, 1, 6>), grid, dim3(256), 0, st, a);
+    else if (a.K <= 512 * kLongPer)
+      hipLaunchKernelGGL((policy_loss_long_kernel<512, 1, 6>), grid, dim3(512), 0, st, a);
+    else if (a.K <= 2 * 512 * kLongPer)
+      hipLaunchKernelGGL((policy_loss_long_kernel<512, 2, 4>), grid, dim3(512), 0, st, a);
+    else
+      hipLaunchKernelGGL((policy_loss_long_kernel<512, 4, 4>), grid, dim3(512), 0, st, a);
+  } else if (a.K % 4) {
+    loss_rows_shape<true>(a.K, rows);
+  } else {
+    loss_rows_shape<false>(a.K, rows);
+  }
   if (a.loss || a.terms)
-    hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(256), 0, st, a.part, (int)grid.x, a.kl_coef, a.entropy_coef,
+    hipLaunchKernelGGL(policy_finish_kernel, dim3(1), dim3(1024), 0, st, a.part, (int)grid.x, a.kl_coef, a.entropy_coef,
                        a.scale, a.loss, a.terms);
   return hipGetLastError();
 }
