@@ -311,3 +311,36 @@ def test_rows_behind_2_31_values(lrb):
     want = ot.policy_loss(tail, ta, host(old[:, -3:]), adv, scale=1.0)
     assert np.all(np.abs(host(grad[-3:]) - want[2]) <= PARTS * want[3] + 1e-40)
     assert not bool(grad[:-3].any())
+
+
+@pytest.mark.parametrize("k,rows", [(2, 700001), (4, 660001), (7, 400003), (16, 330001), (31, 170003), (64, 90001),
+                                    (128, 70001), (255, 36001), (512, 19001), (1000, 9001), (2048, 6301), (3001, 3301),
+                                    (6000, 3101), (12000, 2203)])
+def test_more_tiles_than_workgroups(lrb, k, rows):
+    """Workgroups that take several tiles each: rows that repeat give what the first of them give, bit for bit."""
+    g = rng(13, k)
+    n, s = 97, 3
+    x, a, old, adv, ref = loss_inputs(g, n, k, s, False, True)
+    adv = np.array([0.7, -1.1, 0.4], np.float32)
+    a[1, ::7] = -1
+    noise = g.gumbel(size=(s, n, k)).astype(np.float32)
+    kw = dict(KW, scale=0.5)
+    one = lrb.lr_policy_loss(dev(x), dev(a), dev(old), dev(adv), ref_logp=dev(ref), **kw)
+    first = torch.arange(rows, device="cuda") % n
+    big = [dev(x)[first]] + [dev(t)[:, first].contiguous() for t in (a, old, ref)]
+    loss, terms, grad = lrb.lr_policy_loss(big[0], big[1], big[2], dev(adv), ref_logp=big[3], **kw)
+    assert torch.equal(grad, one[2][first])
+    lp = lrb.lr_policy_logp(big[0], big[1])
+    assert torch.equal(lp, lrb.lr_policy_logp(dev(x), dev(a))[:, first])
+    # the loss's terms: those of the rows that repeat, and of the few behind the last whole round
+    whole, rest = divmod(rows, n)
+    part = lrb.lr_policy_loss(dev(x[:rest]), dev(a[:, :rest]), dev(old[:, :rest]), dev(adv), ref_logp=dev(ref[:, :rest]),
+                              **kw)
+    want = host(one[1]).astype(np.float64) * whole + (host(part[1]) if rest else 0)
+    sizes = ot.policy_loss(x, a, old, adv, ref_logp=ref, **kw)[4] * (whole + 1)
+    assert np.all(np.abs(host(terms) - want) <= PARTS * sizes)
+    if rows * k * s < 3e8:
+        big_noise = dev(noise)[:, first].contiguous()
+        got = lrb.lr_policy_draw(big[0], big_noise)
+        small = lrb.lr_policy_draw(dev(x), dev(noise))
+        assert torch.equal(got[0], small[0][:, first]) and torch.equal(got[1], small[1][:, first])
