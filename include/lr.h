@@ -370,8 +370,8 @@ enum lr_grad_type {
 };
 
 /* Draws levels: d_actions[s][r] = the level j with the largest float32
- * logits[r][j] + noise[s][r][j], the first on ties and scores that are NaN
- * left out (0 where all are): a sample of softmax(logits[r]) when the noise is
+ * logits[r][j] + noise[s][r][j], the first on ties, NaN left out (0 where no
+ * score is above -inf): a sample of softmax(logits[r]) when the noise is
  * Gumbel(0, 1).
  *   d_noise    float32 [samples][count][levels], supplied by the caller
  *   d_levels   nullable, float32 [levels], the device's phase responses
@@ -447,8 +447,10 @@ typedef struct lr_param {
  * call and an eager one agree); 0 for no values.
  *   d_work  lr_grad_norm_workspace_size(num) bytes, aligned to 8
  * Errors: LR_E_ARG (grad_type), LR_E_SIZE (num < 0 or > LR_MAX_PARAMS, a
- * count < 0), LR_E_NULL, LR_E_WORKSPACE, LR_E_ALIAS, LR_E_HIP. */
+ * count < 0, more than LR_MAX_PARAM_VALUES values in all), LR_E_NULL,
+ * LR_E_WORKSPACE, LR_E_ALIAS, LR_E_HIP. */
 #define LR_MAX_PARAMS 65536
+#define LR_MAX_PARAM_VALUES ((int64_t)1 << 40)
 int64_t lr_grad_norm_workspace_size(int32_t num);
 int lr_grad_norm(const lr_param* params, int32_t num, int32_t grad_type, float* d_norm, void* d_work,
                  size_t work_bytes, void* stream);
@@ -481,9 +483,9 @@ int lr_grad_norm(const lr_param* params, int32_t num, int32_t grad_type, float* 
  *     step another seed.  A block in which a moment reaches 2^126 or is not
  *     finite turns to NaN.
  * No two buffers of the call may overlap (gradients may be read twice).
- * Errors: LR_E_SIZE (num < 0 or > LR_MAX_PARAMS, a count < 0, step < 1),
- * LR_E_ARG (types; lr, eps or weight_decay not finite, eps or weight_decay
- * < 0, a beta not in [0, 1), max_norm not > 0), LR_E_NULL, LR_E_ALIAS, LR_E_HIP. */
+ * Errors: LR_E_SIZE (as lr_grad_norm; step < 1), LR_E_ARG (types; lr, eps or
+ * weight_decay not finite, eps or weight_decay < 0, a beta not in [0, 1),
+ * max_norm not > 0), LR_E_NULL, LR_E_ALIAS, LR_E_HIP. */
 #define LR_STATE_BLOCK 256
 enum lr_state_type {
   LR_STATE_F32 = 0,

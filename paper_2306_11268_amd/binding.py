@@ -648,8 +648,10 @@ class TrainTensors:
     params: float32 tensors (None for lr_grad_norm alone); grads: one for each,
     all float32 or all bfloat16.  bits: 32 or 8, of the moments, which are
     allocated as zeros unless m, v (and for 8 bits scales) are given.  The
-    object keeps the tensors' memory; their values may change between steps,
+    object keeps the tensors' memory: their values may change between steps,
     and set_grads puts other gradients in place."""
+
+    _FIELDS = ("d_param", "d_grad", "d_m", "d_v", "d_scales", "count")
 
     def __init__(self, params, grads, bits: int = 32, m=None, v=None, scales=None):
         torch = _torch()
@@ -657,18 +659,18 @@ class TrainTensors:
             raise ValueError("bits must be 8 or 32")
         self.bits = bits
         self.num = len(grads)
-        self._table = (LrParam * max(self.num, 1))()
+        # lr_param [num], field by field
+        self._table = (c_int64 * (len(self._FIELDS) * max(self.num, 1)))()
         self._held = {}
         like = grads if params is None else params
         self.device = like[0].device if self.num else torch.device("cuda", torch.cuda.current_device())
-        self._counts = [int(t.numel()) for t in like]
-        for i, n in enumerate(self._counts):
-            self._table[i].count = n
+        self._counts = [t.numel() for t in like]
+        self._set("count", self._counts)
+        self.params = None
         if params is not None:
             mtype = torch.uint8 if bits == 8 else torch.float32
             new = lambda: [torch.zeros(n, dtype=mtype, device=self.device) for n in self._counts]  # noqa: E731
-            self._hold("d_param", params, torch.float32, self._counts)
-            self.params = list(params)
+            self.params = self._hold("d_param", params, torch.float32, self._counts)
             self.m = self._hold("d_m", new() if m is None else m, mtype, self._counts)
             self.v = self._hold("d_v", new() if v is None else v, mtype, self._counts)
             if bits == 8:
@@ -678,20 +680,23 @@ class TrainTensors:
                 self.scales = self._hold("d_scales", scales, torch.float32, [2 * b for b in blocks])
         self.set_grads(grads)
 
+    def _set(self, field, values) -> None:
+        if self.num:
+            self._table[self._FIELDS.index(field)::len(self._FIELDS)] = values
+
     def _hold(self, field, tensors, dtype, counts):
         """Checks one kind of tensors and puts their addresses into the table."""
         tensors = list(tensors)
         if len(tensors) != len(counts):
             raise ValueError(f"{field}: {len(tensors)} tensors for {len(counts)}")
+        dev = self.device
         for t, n in zip(tensors, counts):
-            if t.device != self.device or not t.is_cuda or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
-                raise ValueError(f"{field}: a contiguous {dtype} tensor of {n} values on {self.device} is needed, "
+            if t.numel() != n or t.dtype != dtype or t.device != dev or not t.is_contiguous() or not t.is_cuda:
+                raise ValueError(f"{field}: a contiguous {dtype} tensor of {n} values on {dev} is needed, "
                                  f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-        # (a second tensor on the same memory keeps it, whatever becomes of the caller's)
-        held = [t.detach() for t in tensors]
-        self._held[field] = held
-        for i, t in enumerate(held):
-            setattr(self._table[i], field, t.data_ptr())
+        # (the memory stays with this object, whatever becomes of the caller's tensors)
+        self._held[field] = [t.untyped_storage() for t in tensors]
+        self._set(field, [t.data_ptr() for t in tensors])
         return tensors
 
     def set_grads(self, grads) -> None:
@@ -699,8 +704,15 @@ class TrainTensors:
         dtype = grads[0].dtype if len(grads) else torch.float32
         if dtype not in (torch.float32, torch.bfloat16):
             raise ValueError(f"gradients must be float32 or bfloat16, got {dtype}")
-        self._hold("d_grad", grads, dtype, self._counts)
+        self.grads = self._hold("d_grad", grads, dtype, self._counts)
         self.grad_type = LR_GRAD_BF16 if dtype == torch.bfloat16 else LR_GRAD_F32
+
+    def first(self):
+        """The first parameter and its gradient, which must be where they were when they were given."""
+        p, g = self.params[0], self.grads[0]
+        if (p.data_ptr(), g.data_ptr()) != (self._table[0], self._table[1]):
+            raise ValueError("a tensor has other memory than when it was given")
+        return p, g
 
 
 def lr_grad_norm(grads, out=None):
@@ -724,7 +736,7 @@ def lr_adamw_update(tensors: TrainTensors, step: int, lr: float, beta1: float = 
     finite leaves everything as it was.  seed (of the rounding of 8-bit
     moments, a 32-bit number) defaults to the step."""
     torch = _torch()
-    if "d_param" not in tensors._held:
+    if tensors.params is None:
         raise ValueError("these tensors have no parameters")
     _check(_run_on(tensors.device, load().lr_adamw_update, tensors._table, tensors.num, tensors.grad_type,
                    LR_STATE_8BIT if tensors.bits == 8 else LR_STATE_F32, int(step), lr, beta1, beta2, eps,
@@ -736,7 +748,7 @@ def lr_adamw_moments(tensors: TrainTensors, out_m=None, out_v=None):
     """The moments as float32, ([m of each tensor], [v of each]): what the codes
     of 8-bit moments stand for, or the tensors themselves where they are float32."""
     torch = _torch()
-    if "d_param" not in tensors._held:
+    if tensors.params is None:
         raise ValueError("these tensors have no parameters")
     if tensors.bits == 32:
         if out_m is not None or out_v is not None:
@@ -765,8 +777,10 @@ def policy_train_step(tensors: TrainTensors, actions, old_logp, advantages, step
     (policy: the arguments of lr_policy_loss) writes their gradient into
     tensors' first gradient, the norm is taken over all gradients, and the
     clipped AdamW step moves every parameter.  Returns (loss, terms, norm)."""
-    logits = tensors.params[0]
-    grad = tensors._held["d_grad"][0].view(logits.shape)
+    if not tensors.params:
+        raise ValueError("these tensors have no parameters")
+    logits, grad = tensors.first()
+    grad = grad.view(logits.shape)
     loss, terms, _ = lr_policy_loss(logits, actions, old_logp, advantages, grad_dtype=grad.dtype, out_grad=grad,
                                     **policy)
     norm = lr_grad_norm(tensors)

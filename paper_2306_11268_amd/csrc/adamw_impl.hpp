@@ -27,15 +27,19 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
 }
 
 // Tensor of the list that chunk c of the launch belongs to.
-__device__ __forceinline__ int tensor_of(const TensorList& l, long long c) {
+template <class F>
+__device__ __forceinline__ int tensor_of(int num, uint32_t c, F&& chunk0) {
   int lo = 0;
-  int hi = l.num;
+  int hi = num;
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
-    if (c >= l.t[mid].chunk0) lo = mid;
+    if (c >= chunk0(mid)) lo = mid;
     else hi = mid;
   }
   return lo;
+}
+__device__ __forceinline__ int tensor_of(const TensorList& l, uint32_t c) {
+  return tensor_of(l.num, c, [&](int i) { return l.t[i].chunk0; });
 }
 
 // Values i .. i + 3 of a tensor, any alignment; FULL: all are there.
@@ -103,28 +107,29 @@ __device__ __forceinline__ void put_codes(void* p, long long i, long long count,
 // ---- norm ------------------------------------------------------------------
 // Squares and sums in float64: no square of a float32 leaves its range.
 template <int THREADS>
-__device__ __forceinline__ double grad_square_sum(const TensorList& l, int bf16, long long chunk, long long step) {
+__device__ __forceinline__ double grad_square_sum(const GradList& l, int bf16, uint32_t chunk, uint32_t step) {
   double s = 0.;
   for (; chunk < l.chunks; chunk += step) {
-    const TensorEntry& t = l.t[tensor_of(l, chunk)];
-    const long long base = (chunk - t.chunk0) * kNormChunk;
+    const int t = tensor_of(l.num, chunk, [&](int i) { return l.chunk0[i]; });
+    const long long base = (long long)(chunk - l.chunk0[t]) * kNormChunk;
+    const long long count = l.count[t];
     auto one = [&](auto full) {
       constexpr int QUADS = kNormChunk / THREADS / 4;
       float v[QUADS][4];
 #pragma unroll
       for (int q = 0; q < QUADS; ++q)
-        quad_grad<decltype(full)::value>(t.grad, bf16, base + 4 * (q * THREADS + (int)threadIdx.x), t.count, v[q]);
+        quad_grad<decltype(full)::value>(l.grad[t], bf16, base + 4 * (q * THREADS + (int)threadIdx.x), count, v[q]);
 #pragma unroll
       for (int q = 0; q < QUADS; ++q)
 #pragma unroll
         for (int j = 0; j < 4; ++j) s += (double)v[q][j] * (double)v[q][j];
     };
-    if (t.count - base >= kNormChunk) one(std::true_type{});
+    if (count - base >= kNormChunk) one(std::true_type{});
     else one(std::false_type{});
   }
   return s;
 }
-__global__ void __launch_bounds__(kOptThreads) grad_norm_kernel(TensorList l, int bf16, double* __restrict__ part) {
+__global__ void __launch_bounds__(kOptThreads) grad_norm_kernel(GradList l, int bf16, double* __restrict__ part) {
   __shared__ double red[kOptThreads / 64];
   const double s = block_sum_d<kOptThreads>(grad_square_sum<kOptThreads>(l, bf16, blockIdx.x, gridDim.x), red);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -139,7 +144,7 @@ __global__ void __launch_bounds__(1024) grad_norm_finish_kernel(const double* __
 // A few chunks: one workgroup, one launch.
 constexpr int kNormOneValues = 32768;
 constexpr int kNormOneThreads = kNormChunk / 4;
-__global__ void __launch_bounds__(kNormOneThreads) grad_norm_one_kernel(TensorList l, int bf16, float* norm) {
+__global__ void __launch_bounds__(kNormOneThreads) grad_norm_one_kernel(GradList l, int bf16, float* norm) {
   __shared__ double red[kNormOneThreads / 64];
   const double s = block_sum_d<kNormOneThreads>(grad_square_sum<kNormOneThreads>(l, bf16, 0, 1), red);
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
@@ -302,9 +307,9 @@ __device__ __forceinline__ void adamw_chunk(const TensorEntry& t, const AdamwArg
 
 template <bool BITS8, bool BF16>
 __global__ void __launch_bounds__(kOptThreads) adamw_kernel(TensorList l, AdamwArgs a) {
-  for (long long c = blockIdx.x; c < l.chunks; c += gridDim.x) {
+  for (uint32_t c = blockIdx.x; c < l.chunks; c += gridDim.x) {
     const TensorEntry& t = l.t[tensor_of(l, c)];
-    const long long base = (c - t.chunk0) * kStepChunk;
+    const long long base = (long long)(c - t.chunk0) * kStepChunk;
     if (t.count - base >= kStepChunk) adamw_chunk<BITS8, BF16, true>(t, a, base);
     else adamw_chunk<BITS8, BF16, false>(t, a, base);
   }
@@ -333,23 +338,23 @@ __device__ __forceinline__ void moments_chunk(const TensorEntry& t, long long ba
   }
 }
 __global__ void __launch_bounds__(kOptThreads) moments_kernel(TensorList l) {
-  for (long long c = blockIdx.x; c < l.chunks; c += gridDim.x) {
+  for (uint32_t c = blockIdx.x; c < l.chunks; c += gridDim.x) {
     const TensorEntry& t = l.t[tensor_of(l, c)];
-    const long long base = (c - t.chunk0) * kStepChunk;
+    const long long base = (long long)(c - t.chunk0) * kStepChunk;
     if (t.count - base >= kStepChunk) moments_chunk<true>(t, base);
     else moments_chunk<false>(t, base);
   }
 }
 
 // ---- launches ----------------------------------------------------------------
-hipError_t launch_grad_norm(const TensorList* lists, int num, int bf16, double* part, float* norm, hipStream_t st) {
+hipError_t launch_grad_norm(const GradList* lists, int num, int bf16, double* part, float* norm, hipStream_t st) {
   if (num == 1 && lists[0].chunks <= kNormOneValues / kNormChunk) {
     hipLaunchKernelGGL(grad_norm_one_kernel, dim3(1), dim3(kNormOneThreads), 0, st, lists[0], bf16, norm);
     return hipGetLastError();
   }
   int parts = 0;
   for (int i = 0; i < num; ++i) {
-    const int grid = (int)std::min<long long>(lists[i].chunks, kNormParts);
+    const int grid = (int)std::min<uint32_t>(lists[i].chunks, kNormParts);
     hipLaunchKernelGGL(grad_norm_kernel, dim3(grid), dim3(kOptThreads), 0, st, lists[i], bf16, part + parts);
     parts += grid;
   }
@@ -359,10 +364,10 @@ hipError_t launch_grad_norm(const TensorList* lists, int num, int bf16, double* 
 
 uint32_t tensor_key(uint32_t seed, uint32_t i) { return mix32(seed + 0x9E3779B9u * i); }
 
-static dim3 chunk_grid(const TensorList& l) { return dim3((unsigned)std::min<long long>(l.chunks, 1 << 22)); }
+static dim3 chunk_grid(const TensorList& l) { return dim3((unsigned)std::min<uint32_t>(l.chunks, 1u << 22)); }
 
 hipError_t launch_adamw(const TensorList& l, const AdamwArgs& a, hipStream_t st) {
-  if (l.chunks <= 0) return hipSuccess;
+  if (l.chunks == 0) return hipSuccess;
   auto go = [&](auto bits8, auto bf16) {
     hipLaunchKernelGGL((adamw_kernel<decltype(bits8)::value, decltype(bf16)::value>), chunk_grid(l), dim3(kOptThreads),
                        0, st, l, a);
@@ -375,7 +380,7 @@ hipError_t launch_adamw(const TensorList& l, const AdamwArgs& a, hipStream_t st)
 }
 
 hipError_t launch_moments(const TensorList& l, hipStream_t st) {
-  if (l.chunks <= 0) return hipSuccess;
+  if (l.chunks == 0) return hipSuccess;
   hipLaunchKernelGGL(moments_kernel, chunk_grid(l), dim3(kOptThreads), 0, st, l);
   return hipGetLastError();
 }

@@ -597,35 +597,51 @@ int params_check(const lr_param* params, int32_t num) {
   if (num > 0 && !params) return LR_E_NULL;
   int64_t all = 0;
   for (int32_t i = 0; i < num; ++i) {
-    if (params[i].count < 0 || params[i].count > kMaxValues - all) return LR_E_SIZE;
+    if (params[i].count < 0 || params[i].count > LR_MAX_PARAM_VALUES - all) return LR_E_SIZE;
     all += params[i].count;
   }
   return LR_OK;
 }
 
+// The list that the next tensor goes into, of those of one launch each.
+static_assert(LR_MAX_PARAM_VALUES / lr::kStepChunk + LR_MAX_PARAMS < (int64_t(1) << 31), "chunks of a launch");
+template <class L>
+L& list_for(std::vector<L>& lists, int most) {
+  if (lists.empty() || lists.back().num == most) lists.push_back(L{});
+  return lists.back();
+}
+
 // The tensors in lists of one launch each, empty ones left out; the random
 // bits' keys count every tensor.
-std::vector<lr::TensorList> tensor_lists(const lr_param* params, int32_t num, uint32_t seed, int chunk) {
+std::vector<lr::TensorList> tensor_lists(const lr_param* params, int32_t num, uint32_t seed) {
   std::vector<lr::TensorList> lists;
   for (int32_t i = 0; i < num; ++i) {
     const lr_param& p = params[i];
     if (p.count == 0) continue;
-    if (lists.empty() || lists.back().num == lr::kTensorsPerLaunch) lists.push_back(lr::TensorList{});
-    lr::TensorList& l = lists.back();
-    lr::TensorEntry& t = l.t[l.num++];
-    t.param = p.d_param;
-    t.grad = p.d_grad;
-    t.m = p.d_m;
-    t.v = p.d_v;
-    t.scales = p.d_scales;
-    t.count = static_cast<long long>(p.count);
-    t.chunk0 = l.chunks;
-    t.key = lr::tensor_key(seed, static_cast<uint32_t>(i));
-    l.chunks += (t.count + chunk - 1) / chunk;
+    const int64_t chunks = (p.count + lr::kStepChunk - 1) / lr::kStepChunk;
+    lr::TensorList& l = list_for(lists, lr::kTensorsPerLaunch);
+    l.t[l.num++] = {p.d_param, p.d_grad, p.d_m, p.d_v, p.d_scales, static_cast<long long>(p.count), l.chunks,
+                    lr::tensor_key(seed, static_cast<uint32_t>(i))};
+    l.chunks += static_cast<uint32_t>(chunks);
+  }
+  return lists;
+}
+std::vector<lr::GradList> grad_lists(const lr_param* params, int32_t num) {
+  std::vector<lr::GradList> lists;
+  for (int32_t i = 0; i < num; ++i) {
+    const lr_param& p = params[i];
+    if (p.count == 0) continue;
+    const int64_t chunks = (p.count + lr::kNormChunk - 1) / lr::kNormChunk;
+    lr::GradList& l = list_for(lists, lr::kGradsPerLaunch);
+    l.grad[l.num] = p.d_grad;
+    l.count[l.num] = static_cast<long long>(p.count);
+    l.chunk0[l.num++] = l.chunks;
+    l.chunks += static_cast<uint32_t>(chunks);
   }
   return lists;
 }
 
+static_assert(LR_MAX_ROLLOUTS <= lr::kMaxRollouts, "rollouts of a call");
 static_assert(LR_STATE_BLOCK == lr::kStateBlock, "block of the 8-bit moments");
 size_t scale_bytes(int64_t count) { return static_cast<size_t>((count + LR_STATE_BLOCK - 1) / LR_STATE_BLOCK) * 8; }
 
@@ -1345,7 +1361,7 @@ int lr_policy_draw(const float* d_logits, const float* d_noise, const float* d_l
   hipStream_t st = static_cast<hipStream_t>(stream);
   const lr::PolicyDrawArgs a{d_logits, d_noise, d_levels, samples, levels, static_cast<long long>(count),
                              d_actions, d_logp, d_phi};
-  return run_timed("policy_draw", st, [&] { return lr::launch_policy_draw(a, st); });
+  return no_throw([&] { return run_timed("policy_draw", st, [&] { return lr::launch_policy_draw(a, st); }); });
 }
 
 int lr_policy_logp(const float* d_logits, const int32_t* d_actions, int32_t samples, int64_t count, int32_t levels,
@@ -1361,7 +1377,7 @@ int lr_policy_logp(const float* d_logits, const int32_t* d_actions, int32_t samp
   hipStream_t st = static_cast<hipStream_t>(stream);
   const lr::PolicyDrawArgs a{d_logits, nullptr, nullptr, samples, levels, static_cast<long long>(count),
                              const_cast<int32_t*>(d_actions), d_logp, nullptr};
-  return run_timed("policy_logp", st, [&] { return lr::launch_policy_draw(a, st); });
+  return no_throw([&] { return run_timed("policy_logp", st, [&] { return lr::launch_policy_draw(a, st); }); });
 }
 
 int64_t lr_policy_workspace_size(void) { return static_cast<int64_t>(lr::kPolicyParts) * 4 * sizeof(double); }
@@ -1395,12 +1411,12 @@ int lr_policy_loss(const lr_policy* policy, const float* d_logits, const int32_t
                              levels, grad_type == LR_GRAD_BF16 ? 1 : 0, static_cast<long long>(count),
                              policy->clip_low, policy->clip_high, policy->kl_coef, policy->entropy_coef,
                              policy->scale, d_grad_logits, d_loss, d_terms, static_cast<double*>(d_work)};
-  return run_timed("policy_loss", st, [&] { return lr::launch_policy_loss(a, st); });
+  return no_throw([&] { return run_timed("policy_loss", st, [&] { return lr::launch_policy_loss(a, st); }); });
 }
 
 int64_t lr_grad_norm_workspace_size(int32_t num) {
   if (num < 0 || num > LR_MAX_PARAMS) return -static_cast<int64_t>(LR_E_SIZE);
-  const int64_t lists = std::max<int64_t>(1, (num + lr::kTensorsPerLaunch - 1) / lr::kTensorsPerLaunch);
+  const int64_t lists = std::max<int64_t>(1, (num + lr::kGradsPerLaunch - 1) / lr::kGradsPerLaunch);
   return lists * lr::kNormParts * static_cast<int64_t>(sizeof(double));
 }
 
@@ -1421,7 +1437,7 @@ int lr_grad_norm(const lr_param* params, int32_t num, int32_t grad_type, float* 
   }
   return no_throw([&] {
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const std::vector<lr::TensorList> lists = tensor_lists(params, num, 0, lr::kNormChunk);
+    const std::vector<lr::GradList> lists = grad_lists(params, num);
     return run_timed("grad_norm", st, [&] {
       return lr::launch_grad_norm(lists.data(), static_cast<int>(lists.size()), grad_type == LR_GRAD_BF16 ? 1 : 0,
                                   static_cast<double*>(d_work), d_norm, st);
@@ -1475,7 +1491,7 @@ int lr_adamw_update(const lr_param* params, int32_t num, int32_t grad_type, int3
     a.bf16 = grad_type == LR_GRAD_BF16 ? 1 : 0;
     a.bits8 = bits8 ? 1 : 0;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const std::vector<lr::TensorList> lists = tensor_lists(params, num, seed, lr::kStepChunk);
+    const std::vector<lr::TensorList> lists = tensor_lists(params, num, seed);
     return run_timed(bits8 ? "adamw8" : "adamw", st, [&] {
       for (const lr::TensorList& l : lists) {
         const hipError_t e = lr::launch_adamw(l, a, st);
@@ -1508,7 +1524,7 @@ int lr_adamw_moments(const lr_param* params, int32_t num, float* const* d_m_out,
     }
     if (ranges_alias(ranges)) return LR_E_ALIAS;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const std::vector<lr::TensorList> lists = tensor_lists(outs.data(), num, 0, lr::kStepChunk);
+    const std::vector<lr::TensorList> lists = tensor_lists(outs.data(), num, 0);
     return run_timed("adamw_moments", st, [&] {
       for (const lr::TensorList& l : lists) {
         const hipError_t e = lr::launch_moments(l, st);

@@ -254,6 +254,7 @@ struct PolicyDrawArgs {
 };
 hipError_t launch_policy_draw(const PolicyDrawArgs& a, hipStream_t st);
 
+constexpr int kMaxRollouts = 1024;  // samples of a loss
 constexpr int kPolicyParts = 2048;  // workgroups of the loss kernel, four partial sums each
 struct PolicyLossArgs {
   const float* logits;
@@ -275,11 +276,14 @@ struct PolicyLossArgs {
 hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st);
 
 // The tensors of one launch of an optimiser step, worked in chunks of so many
-// values (a kernel argument: a launch may be captured).
+// values (a kernel argument: a launch may be captured, and hundreds of tensors
+// take a few launches).  chunk0: the tensor's first chunk of the launch's, which
+// are fewer than 2^31.
 constexpr int kNormChunk = 4096;
 constexpr int kStepChunk = 1024;  // of lr_adamw_update and lr_adamw_moments
 constexpr int kStateBlock = 256;  // values that share the scales of 8-bit moments
-constexpr int kTensorsPerLaunch = 60;
+constexpr int kTensorsPerLaunch = 68;
+constexpr int kGradsPerLaunch = 198;
 struct TensorEntry {
   float* param;
   const void* grad;
@@ -287,16 +291,23 @@ struct TensorEntry {
   void* v;
   float* scales;
   long long count;
-  long long chunk0;  // first chunk
-  uint32_t key;      // of the random bits
+  uint32_t chunk0;
+  uint32_t key;  // of the random bits
 };
 struct TensorList {
   TensorEntry t[kTensorsPerLaunch];
-  long long chunks;
+  uint32_t chunks;
+  int num;
+};
+struct GradList {
+  const void* grad[kGradsPerLaunch];
+  long long count[kGradsPerLaunch];
+  uint32_t chunk0[kGradsPerLaunch];
+  uint32_t chunks;
   int num;
 };
 constexpr int kNormParts = 2048;  // partial sums of one launch
-hipError_t launch_grad_norm(const TensorList* lists, int num, int bf16, double* part, float* norm, hipStream_t st);
+hipError_t launch_grad_norm(const GradList* lists, int num, int bf16, double* part, float* norm, hipStream_t st);
 struct AdamwArgs {
   const float* norm;  // nullable
   float max_norm;
@@ -308,7 +319,7 @@ struct AdamwArgs {
   int bf16;
   int bits8;
 };
-static_assert(sizeof(TensorList) + sizeof(AdamwArgs) + 64 <= 4096, "kernel arguments");
+static_assert(sizeof(TensorList) + sizeof(AdamwArgs) <= 4096 && sizeof(GradList) + 32 <= 4096, "kernel arguments");
 hipError_t launch_adamw(const TensorList& l, const AdamwArgs& a, hipStream_t st);
 // m and v of 8-bit moments as float32 (into param and grad of the entries).
 hipError_t launch_moments(const TensorList& l, hipStream_t st);

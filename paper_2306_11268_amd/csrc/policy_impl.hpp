@@ -244,7 +244,6 @@ __device__ __forceinline__ void running_join(Running& w, float* red) {
 constexpr int kLongThreads = 512;
 constexpr int kLongPer = 16;                           // values a thread has in flight
 constexpr int kLongStep = kLongThreads * kLongPer;     // values of a round
-constexpr int kMaxRollouts = 1024;                     // of a call
 constexpr int kLongSamples = 4;                        // rollouts that one pass over the logits serves
 
 __global__ void __launch_bounds__(kLongThreads) policy_draw_long_kernel(PolicyDrawArgs a) {

@@ -269,10 +269,13 @@ def test_tensors_behind_2_32_values(lrb):
 def test_the_object_keeps_the_memory_it_was_given(lrb):
     p, gr = torch.ones(1000, device="cuda"), torch.ones(1000, device="cuda")
     t = lrb.TrainTensors([p], [gr])
-    keep = t._held["d_param"][0]
     p.data = torch.zeros(1000, device="cuda")  # the caller's tensor goes elsewhere
+    held = t._held["d_param"][0]
     lrb.lr_adamw_update(t, 1, lr=0.1)
-    assert float(p.abs().max()) == 0 and float(keep[0]) < 1
+    keep = torch.empty(0, device="cuda").set_(held)
+    assert float(p.abs().max()) == 0 and keep.numel() == 1000 and float(keep.max()) < 1
+    with pytest.raises(ValueError):
+        lrb.policy_train_step(t, torch.zeros((1, 1), dtype=torch.int32, device="cuda"), gr, gr, 1, lr=0.1)
     with pytest.raises(ValueError):
         t.set_grads([torch.ones(999, device="cuda")])
     with pytest.raises(ValueError):

@@ -79,7 +79,7 @@ def test_a_step_from_rollouts_in_the_emulator(lrb, bits):
     assert np.allclose(flat(host(logp)), want_lp, atol=1e-5)
     # (the first step after a draw: every ratio is 1, and the clipped term is minus the advantages' mean)
     assert abs(float(loss) - o[0]) <= 1e-6 and float(terms[3]) == 0
-    g = host(t._held["d_grad"][0]).reshape(-1, k)
+    g = host(t.grads[0]).reshape(-1, k)
     assert np.linalg.norm(g - o[2]) <= 2e-5 * np.linalg.norm(o[2])
     assert abs(float(norm) - ot.grad_norm([g])) <= 1e-6 * ot.grad_norm([g])
     z = np.zeros(scores.size, np.float32)
@@ -107,7 +107,7 @@ def make_step(lrb, dtype=torch.bfloat16, bits=8):
                                     entropy_coef=0.01, max_norm=0.05)
         return (a, lp, phi, *out, x, bias, t.m[0], t.v[0])
 
-    return step, (x, bias, *t.m, *t.v, *getattr(t, "scales", []), *t._held["d_grad"])
+    return step, (x, bias, *t.m, *t.v, *getattr(t, "scales", []), *t.grads)
 
 
 @pytest.mark.parametrize("bits,dtype", [(8, torch.bfloat16), (32, torch.float32)])
@@ -162,5 +162,5 @@ def test_rewards_move_the_policy_towards_the_better_level(lrb):
     adv = (a == 3).float()
     adv = (adv - adv.mean()).contiguous()
     lrb.policy_train_step(t, a, lp, adv, 1, lr=0.1)
-    g = host(t._held["d_grad"][0])
+    g = host(t.grads[0])
     assert np.all(g[:, 3] < 0) and np.all(host(x)[:, 3] > 0)
