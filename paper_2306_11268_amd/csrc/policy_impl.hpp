@@ -607,7 +607,11 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
       if (act >= 0) {
         made += 1.f;
         slopes += c.y;
-        if (act < K) __hip_atomic_fetch_add(row_add + act, c.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        if (act >= K) return;
+        // (a place of this lane alone.  Where it has all of a row's rollouts, the atomic lets it go on without
+        // the sum; where every lane adds, the atomics' rate holds the pass: 612500 x 16, 32 rollouts 132 -> 82 us)
+        if (DIRECT) row_add[act] += c.y;
+        else __hip_atomic_fetch_add(row_add + act, c.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
       }
     };
     if constexpr (DIRECT) {
