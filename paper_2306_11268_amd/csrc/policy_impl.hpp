@@ -125,10 +125,12 @@ __device__ __forceinline__ float exp_fast(float x) { return __builtin_amdgcn_exp
 // keeps it.)
 __device__ __forceinline__ float floor_d(float d) { return fmaxf(d, -1e30f); }
 
-__device__ __forceinline__ uint16_t bf16_bits(float x) {
-  const uint32_t u = __float_as_uint(x);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((u >> 16) | 0x40);  // (a NaN stays one)
-  return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
+// Two values rounded to bf16, nearest even (gfx950 converts them in one
+// instruction; in integer arithmetic it was six a value).
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2){a, b}, b2));
 }
 
 // ---- draw ------------------------------------------------------------------
@@ -454,13 +456,18 @@ __device__ __forceinline__ double wave_sum_exp_d(const float* row, int K, float 
   return lanes_sum_d<64>(sum_exp_d<64>(row, K, threadIdx.x & 63, m));
 }
 // dL/dlogit = (sum of the slopes of choices of this level) - p (all slopes -
-// w (log p + H)), w = scale * entropy_coef * choices made.
-__device__ __forceinline__ float grad_value(float acc, float e, float d, float inv_z, float lz, float h, float slopes,
-                                            float w) {
-  return acc - e * inv_z * (slopes - w * ((d - lz) + h));
-}
+// w (log p + H)), w = scale * entropy_coef * choices made, p = e / z and
+// log p = d - lz: acc - e / z (base - w d) with the row's base.
+struct RowGrad {
+  float base, w, inv_z;
+  __device__ __forceinline__ RowGrad(const PolicyLossArgs& a, float slopes, float made, float inv_z_, float lz, float h)
+      : w(a.scale * a.entropy_coef * made), inv_z(inv_z_) {
+    base = slopes - w * (h - lz);
+  }
+  __device__ __forceinline__ float at(float acc, float e, float d) const { return acc - (e * inv_z) * (base - w * d); }
+};
 __device__ __forceinline__ void grad_store(void* grad, int bf16, long long at, float g) {
-  if (bf16) static_cast<uint16_t*>(grad)[at] = bf16_bits(g);
+  if (bf16) static_cast<uint16_t*>(grad)[at] = (uint16_t)bf16_pair(g, 0.f);
   else static_cast<float*>(grad)[at] = g;
 }
 // Columns c .. c + 3 of a row that starts at `row` in the gradient.
@@ -468,7 +475,7 @@ template <bool TAIL>
 __device__ __forceinline__ void quad_store(void* grad, int bf16, long long row, int K, int c, const float* g) {
   if (!TAIL || c + 4 <= K) {
     if (bf16) {
-      const QuadBf16 q{{bf16_bits(g[0]) | (uint32_t)bf16_bits(g[1]) << 16, bf16_bits(g[2]) | (uint32_t)bf16_bits(g[3]) << 16}};
+      const QuadBf16 q{{bf16_pair(g[0], g[1]), bf16_pair(g[2], g[3])}};
       *reinterpret_cast<QuadBf16*>(static_cast<uint16_t*>(grad) + row + c) = q;
     } else {
       *reinterpret_cast<Quad*>(static_cast<float*>(grad) + row + c) = Quad{{g[0], g[1], g[2], g[3]}};
@@ -656,7 +663,7 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
         all.x += sums[p][row].x;
         all.y += sums[p][row].y;
       }
-      const float w = a.scale * a.entropy_coef * all.y;
+      const RowGrad to(a, all.x, all.y, inv_z, lz, h);
 #pragma unroll
       for (int i = 0; i < N; i += 4) {
         const int c = quad_col<G>(lane, i);
@@ -671,7 +678,7 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
         float g[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          g[j] = all.y > 0.f ? grad_value(s[j], exp_fast(d[i + j]), d[i + j], inv_z, lz, h, all.x, w) : 0.f;
+          g[j] = all.y > 0.f ? to.at(s[j], exp_fast(d[i + j]), d[i + j]) : 0.f;
         if (ok) quad_store<TAIL>(a.grad, a.bf16, (r0 + row) * K, K, c, g);
       }
     }
@@ -776,12 +783,12 @@ __global__ void __launch_bounds__(THREADS, WAVES) policy_loss_long_kernel(Policy
       }
       slopes = lanes_reduce<64>(slopes, OpSum{});
       made = lanes_reduce<64>(made, OpSum{});
-      const float w = a.scale * a.entropy_coef * made;
+      const RowGrad to(a, slopes, made, inv_z, lz, h);
       auto write = [&](float (&x)[kLongPer], int k0) {
 #pragma unroll
         for (int i = 0; i < kLongPer; ++i) {
           const float d = x[i] - m;
-          x[i] = made > 0.f ? grad_value(0.f, exp_fast(d), floor_d(d), inv_z, lz, h, slopes, w) : 0.f;
+          x[i] = made > 0.f ? to.at(0.f, exp_fast(d), floor_d(d)) : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < kLongPer; i += 4)
@@ -811,7 +818,7 @@ __global__ void __launch_bounds__(THREADS, WAVES) policy_loss_long_kernel(Policy
         }
         if (!first) continue;
         const float d = (s == tid ? x0 : row[act]) - m;
-        grad_store(a.grad, a.bf16, r * K + act, grad_value(g, exp_fast(d), floor_d(d), inv_z, lz, h, slopes, w));
+        grad_store(a.grad, a.bf16, r * K + act, to.at(g, exp_fast(d), floor_d(d)));
       }
     }
     __syncthreads();
