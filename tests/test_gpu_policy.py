@@ -344,3 +344,26 @@ def test_more_tiles_than_workgroups(lrb, k, rows):
         got = lrb.lr_policy_draw(big[0], big_noise)
         small = lrb.lr_policy_draw(dev(x), dev(noise))
         assert torch.equal(got[0], small[0][:, first]) and torch.equal(got[1], small[1][:, first])
+
+
+@pytest.mark.parametrize("k", (2, 16, 100, 256, 1024, 2000, 3000, 5000, 12000, 40007))
+@pytest.mark.parametrize("low", (-np.inf, float(np.finfo(np.float32).min), -1e30, -200.0))
+def test_levels_barred_by_very_low_scores(lrb, k, low):
+    """Most levels far below the others, in runs as long as a thread's share of a row: nothing of them is left."""
+    g = rng(14, k)
+    r, s = 5, 4
+    x, a, old, adv, ref = loss_inputs(g, r, k, s, True, True)
+    keep = np.zeros((r, k), bool)
+    keep[np.arange(r)[None, :], a] = True
+    keep[:, -1] = True
+    x = np.where(keep, x, np.float32(low))
+    x[3] = np.where(keep[3], x[3] + np.float32(50), x[3])
+    lp = ot.policy_logp(x, a)
+    old, ref = (lp + 0.1).astype(np.float32), (lp - 0.2).astype(np.float32)
+    _, terms, grad = check_loss(lrb, x, a, old, adv, ref)
+    assert np.isfinite(host(grad)).all() and np.isfinite(host(terms)).all()
+    check_logp(x, a, host(lrb.lr_policy_logp(dev(x), dev(a))))
+    noise = g.gumbel(size=(2, r, k)).astype(np.float32)
+    got, glp, _ = lrb.lr_policy_draw(dev(x), dev(noise))
+    assert np.array_equal(host(got), ot.policy_draw(x, noise))
+    check_logp(x, host(got), host(glp))
