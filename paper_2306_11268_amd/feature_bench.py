@@ -16,7 +16,13 @@ seeded synthetic workloads; the optics are those of the workloads named.
   architectures (§5.6): the 3-channel DONN's training step (batch 500), the
       codesign layer over 5x200x200 pixels and 256 device levels, and the
       segmentation DONN's training step (5 layers on the paper's 350x350
-      grid, skip field and layer norm, batch 64).
+      grid, skip field and layer norm, batch 64);
+  training device levels by reward: the levels of four rollouts drawn and the
+      policy loss of sixteen over the codesign scores above, the loss of 32
+      over 5x350x350 pixels of a 16-level device, the gradient norm and the
+      AdamW step with 8-bit moments over 5x350x350x256 scores with bf16
+      gradients, the AdamW step over the masks of three channels, and a whole
+      step: draw, the rollouts in the emulator (batch 64), loss, norm, AdamW.
 """
 
 from __future__ import annotations
@@ -127,6 +133,50 @@ def main(argv=None):
     ms = _time(lambda: lb.lr_codesign_backward(scores, noise, levels, 0.5, gphi), K, W)
     nbytes = px * lev * 12 + px * 4
     _line("codesign_backward_256_levels", ms, pixels=px, bytes=nbytes, gbps=nbytes / ms / 1e6)
+
+    # ---- training device levels by reward
+    def rollouts(logits, samples):
+        k = logits.shape[-1]
+        a = torch.randint(0, k, (samples, *logits.shape[:-1]), dtype=torch.int32, device="cuda")
+        lp = lb.lr_policy_logp(logits, a)
+        return a, lp + 0.1 * torch.randn_like(lp), torch.randn(samples, device="cuda"), lp - 0.1
+
+    draws = torch.rand((4, *shape, lev), device="cuda").clamp_(1e-12, 1 - 2.0 ** -24).log_().neg_().log_().neg_()
+    ms = _time(lambda: lb.lr_policy_draw(scores, draws, levels), K, W)
+    nbytes = px * lev * 4 * 5 + px * 4 * 12
+    _line("policy_draw_256_levels_s4", ms, pixels=px, bytes=nbytes, gbps=nbytes / ms / 1e6)
+    for name, logits, s_, side in (("policy_loss_256_levels_s16", scores, 16, 12),
+                                   ("policy_loss_16_levels_s32", torch.randn((5, 350, 350, 16), device="cuda"), 32, 12)):
+        a_, old, adv, ref = rollouts(logits, s_)
+        gl = torch.empty_like(logits)
+        ms = _time(lambda: lb.lr_policy_loss(logits, a_, old, adv, ref_logp=ref, kl_coef=0.05, entropy_coef=0.01,
+                                             out_grad=gl), K, W)
+        nbytes = logits.numel() * 8 + old.numel() * side
+        _line(name, ms, pixels=old.numel() // s_, bytes=nbytes, gbps=nbytes / ms / 1e6)
+    big = torch.zeros((5, 350, 350, lev), device="cuda")
+    t8 = lb.TrainTensors([big], [torch.full_like(big, 1e-3, dtype=torch.bfloat16)], bits=8)
+    ms = _time(lambda: lb.lr_grad_norm(t8), K, W)
+    _line("grad_norm_bf16", ms, elements=big.numel(), bytes=2 * big.numel(), gbps=2 * big.numel() / ms / 1e6)
+    norm = lb.lr_grad_norm(t8)
+    ms = _time(lambda: lb.lr_adamw_update(t8, 7, lr=0.01, norm=norm, max_norm=1.0), K, W)
+    _line("adamw_8_bit_moments", ms, elements=big.numel(), bytes=14 * big.numel(), gbps=14 * big.numel() / ms / 1e6)
+    del big, t8
+    masks = [torch.zeros((w.layers, w.n, w.n), device="cuda") for _ in range(3)]
+    t32 = lb.TrainTensors(masks, [torch.full_like(q, 1e-3) for q in masks])
+    ms = _time(lambda: lb.lr_adamw_update(t32, 7, lr=0.5), K, W)
+    nbytes = 3 * masks[0].numel() * 28
+    _line("adamw_3_channels", ms, elements=3 * masks[0].numel(), bytes=nbytes, gbps=nbytes / ms / 1e6)
+    tp = lb.TrainTensors([scores.clone()], [torch.empty_like(scores, dtype=torch.bfloat16)], bits=8)
+    few, few_labels = amp[:64].contiguous(), labels[:64].contiguous()
+
+    def reward_step():
+        acts, lp, masks4 = lb.lr_policy_draw(tp.params[0], draws, levels)
+        loss4 = torch.stack([lb.lr_loss(lb.lr_donn_forward(net, few, q)["sums"], few_labels)[0] for q in masks4])
+        lb.policy_train_step(tp, acts, lp, loss4.mean() - loss4, 3, lr=0.01, entropy_coef=0.01)
+
+    ms = _time(reward_step, K, W)
+    _line("reward_step_256_levels_s4", ms, pixels=px, rollouts=4, batch=64)
+    del tp, draws
 
     # ---- segmentation DONN: 5 layers on the 350 x 350 grid, batch 64
     ws = wl.scaled(wl.WORKLOADS[3], n=350)
