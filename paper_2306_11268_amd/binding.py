@@ -560,6 +560,8 @@ def _policy_shapes(logits, samples: int):
         raise ValueError("logits must be a device tensor [..., levels]")
     k = int(logits.shape[-1])
     rows = logits.shape[:-1]
+    if k > LR_MAX_CHOICES or samples > LR_MAX_ROLLOUTS:  # (beyond 32 bits, too)
+        raise ValueError(f"at most {LR_MAX_CHOICES} levels and {LR_MAX_ROLLOUTS} rollouts, got {k} and {samples}")
     return rows.numel(), k, (samples, *rows)
 
 
@@ -624,8 +626,13 @@ def lr_policy_loss(logits, actions, old_logp, advantages, ref_logp=None, clip_lo
         raise ValueError(f"grad_dtype must be float32 or bfloat16, got {grad_dtype}")
     if want_grad and out_grad is None:
         out_grad = torch.empty(logits.shape, dtype=grad_dtype, device=dev)
-    loss = torch.empty((), dtype=torch.float32, device=dev) if want_loss else None
-    terms = torch.empty(4, dtype=torch.float32, device=dev) if want_loss else None
+    new = torch.empty
+    if s * count == 0:  # the call enqueues nothing: the loss and the gradient of no choices
+        new = torch.zeros
+        if out_grad is not None:
+            out_grad.zero_()
+    loss = new((), dtype=torch.float32, device=dev) if want_loss else None
+    terms = new(4, dtype=torch.float32, device=dev) if want_loss else None
     work = torch.empty(int(load().lr_policy_workspace_size()), dtype=torch.uint8, device=dev)
     policy = LrPolicy(clip_low, clip_high, kl_coef, entropy_coef, 1.0 / max(1, s * count) if scale is None else scale)
     _check(_run_on(dev, load().lr_policy_loss, ctypes.byref(policy),
@@ -738,6 +745,8 @@ def lr_adamw_update(tensors: TrainTensors, step: int, lr: float, beta1: float = 
     torch = _torch()
     if tensors.params is None:
         raise ValueError("these tensors have no parameters")
+    if step >= 1 << 31:
+        raise ValueError(f"step {step} is beyond 32 bits")
     _check(_run_on(tensors.device, load().lr_adamw_update, tensors._table, tensors.num, tensors.grad_type,
                    LR_STATE_8BIT if tensors.bits == 8 else LR_STATE_F32, int(step), lr, beta1, beta2, eps,
                    weight_decay, _at(tensors.device, norm, torch.float32, (), "norm"), max_norm,

@@ -289,3 +289,18 @@ def test_the_object_keeps_the_memory_it_was_given(lrb):
     same = torch.ones(1000, device="cuda")
     with pytest.raises(lrb.LrError):
         lrb.lr_adamw_update(lrb.TrainTensors([same, same], [gr, gr]), 1, lr=0.1)
+
+
+def test_a_step_beyond_32_bits_is_refused(lrb):
+    p = torch.ones(8, device="cuda")
+    t = lrb.TrainTensors([p], [torch.ones(8, device="cuda")])
+    with pytest.raises(ValueError):
+        lrb.lr_adamw_update(t, 2 ** 32 + 1, lr=0.1)
+    with pytest.raises(lrb.LrError):
+        lrb.lr_adamw_update(t, 0, lr=0.1)
+    assert bool((p == 1).all())
+    lrb.lr_adamw_update(t, 2 ** 31 - 1, lr=0.5)
+    # m = 1 - beta1, v = 1 - beta2, uncorrected, with the call's float32 betas (1 - float32(0.999) is 1.3e-5 below 0.001,
+    # the step 1.58 times half of that: 1.0e-5)
+    b1, b2 = float(np.float32(0.9)), float(np.float32(0.999))
+    assert abs(float(p[0]) - (1 - 0.5 * (1 - b1) / ((1 - b2) ** 0.5 + 1e-8))) < 16 * 2 ** -24

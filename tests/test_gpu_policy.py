@@ -280,6 +280,32 @@ def test_empty_calls_do_nothing(lrb):
     assert a.shape == (0, 5) and lrb.lr_policy_logp(x, a).shape == (0, 5)
 
 
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("rollouts,pixels", [(0, 5), (3, 0), (0, 0)])
+def test_a_loss_of_no_choices_is_zero(lrb, dtype, rollouts, pixels):
+    """Also where the outputs' memory held something else: the step that follows takes them as they are."""
+    x = torch.ones((pixels, 16), device="cuda")
+    a = torch.zeros((rollouts, pixels), dtype=torch.int32, device="cuda")
+    old, adv = torch.zeros((rollouts, pixels), device="cuda"), torch.ones(rollouts, device="cuda")
+    out = torch.full((pixels, 16), 3.0, dtype=dtype, device="cuda")
+    loss, terms, grad = lrb.lr_policy_loss(x, a, old, adv, grad_dtype=dtype, out_grad=out)
+    assert float(loss) == 0 and not bool(terms.any()) and grad is out and not bool(grad.any())
+    assert not bool(lrb.lr_policy_loss(x, a, old, adv, grad_dtype=dtype)[2].any())
+
+
+def test_too_many_levels_or_rollouts_are_refused(lrb):
+    x = torch.zeros((1, 65537), device="cuda")
+    a = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        lrb.lr_policy_draw(x, x[None])
+    with pytest.raises(ValueError):
+        lrb.lr_policy_logp(x, a)
+    with pytest.raises(ValueError):
+        lrb.lr_policy_loss(x, a, a.float(), torch.ones(1, device="cuda"))
+    with pytest.raises(ValueError):
+        lrb.lr_policy_logp(x[:, :16].contiguous(), a.expand(1025, 1).contiguous())
+
+
 def test_shapes_of_masks_pass_through(lrb):
     g = rng(11)
     x = g.standard_normal((2, 5, 7, 12)).astype(np.float32)
