@@ -7,7 +7,11 @@
 // values, four neighbours a lane, which is also a block of the 8-bit moments:
 // its largest exponents are found in the wave.  Nothing is read or written
 // twice: 28 bytes a value with float32 moments and gradients, 14 with 8-bit
-// moments and bf16 gradients.
+// moments and bf16 gradients.  Memory bounds them (a large copy: 5.0 TB/s):
+// 165 M values with 8-bit moments 440 us (5.2 TB/s), their moments written out
+// 262 us (6.3 TB/s, mostly stores), the norm of as many bf16 gradients 60 us
+// (5.5 TB/s); 200 tensors of together 22.2 M values with float32 moments, three
+// launches, 131 us (4.7 TB/s).
 #pragma once
 
 #include "kernels.hpp"

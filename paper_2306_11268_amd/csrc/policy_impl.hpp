@@ -8,7 +8,7 @@
 // A longer row takes a workgroup.  Memory bounds them (a large copy reaches 5.0
 // TB/s on this card): draws of four rollouts for 200000 x 256 logits 180 us (5.7
 // TB/s, reading only), log-probabilities of eight for 612500 x 64 43 us, the
-// loss and gradient of 16 rollouts for 200000 x 256 98 us (4.6 TB/s).
+// loss and gradient of 16 rollouts for 200000 x 256 97 us (4.6 TB/s).
 #pragma once
 
 #include "kernels.hpp"
@@ -948,7 +948,8 @@ hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) {
   if (a.K > kPolicyRowMax) {
     grid = dim3((unsigned)std::min<long long>(a.count, kPolicyParts));
     // (as many rounds held as the row has, up to four: 1500 rows of 65536 levels 210 -> 195 us from one to
-    // four, 6000 of 16384 179 -> 168 from one to two, but 205 with four, whose registers it does not fill)
+    // four, 6000 of 16384 179 -> 168 from one to two, but 205 with four, whose registers it does not fill; 1024
+    // threads, which hold such rows whole but fill a CU alone: 1600 of 40007 139 -> 149, 1500 of 65536 200 -> 200)
     if (a.K <= 256 * kLongPer)
       hipLaunchKernelGGL((policy_loss_long_kernel<256, 1, 6>), grid, dim3(256), 0, st, a);
     else if (a.K <= 512 * kLongPer)
