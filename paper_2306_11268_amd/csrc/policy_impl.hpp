@@ -60,19 +60,24 @@ __device__ __forceinline__ double lanes_sum_d(double x) {
   return x;
 }
 
-// Over a workgroup of THREADS, in a fixed order; red: THREADS / 64 values.  The
-// last barrier leaves red free for the next call.
-template <int THREADS, class Op>
-__device__ __forceinline__ float block_reduce(float x, Op op, float* red) {
-  x = lanes_reduce<64>(x, op);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = red[0];
+// N values over a workgroup of THREADS, in a fixed order.  One barrier: red is
+// free for the next call only behind another one.
+template <int THREADS, int N, class Op>
+__device__ __forceinline__ void block_reduce(float (&x)[N], Op op, float (&red)[N][THREADS / 64]) {
 #pragma unroll
-  for (int i = 1; i < THREADS / 64; ++i) x = op(x, red[i]);
+  for (int i = 0; i < N; ++i) {
+    x[i] = lanes_reduce<64>(x[i], op);
+    if ((threadIdx.x & 63) == 0) red[i][threadIdx.x >> 6] = x[i];
+  }
   __syncthreads();
-  return x;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    x[i] = red[i][0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) x[i] = op(x[i], red[i][w]);
+  }
 }
+// (red: THREADS / 64 values, free again at the end)
 template <int THREADS>
 __device__ __forceinline__ double block_sum_d(double x, double* red) {
   x = lanes_sum_d<64>(x);
@@ -258,48 +263,61 @@ struct Running {
     }
   }
 };
-// Joined over the workgroup: every thread ends with the row's.
-template <int THREADS>
-__device__ __forceinline__ void running_join(Running& w, float* red) {
-  w.rescale(block_reduce<THREADS>(w.m, OpMax{}, red));
-  w.z = block_reduce<THREADS>(w.z, OpSum{}, red);
-  w.zd = block_reduce<THREADS>(w.zd, OpSum{}, red);
-}
 
-constexpr int kLongThreads = 512;
-constexpr int kLongPer = 16;                           // values a thread has in flight
-constexpr int kLongStep = kLongThreads * kLongPer;     // values of a round
-constexpr int kLongSamples = 4;                        // rollouts that one pass over the logits serves
+// Threads of a row's workgroup, and values that each has in flight: with 512 of
+// 16, rows of little more than 2048 levels leave most threads idle, and waves
+// wait at the barriers (four rollouts of 10000 x 2500: 217 us against 110 with 256
+// of 8, 10000 x 5000 227 against 183); longer ones need the bytes in flight when
+// there are few of them (eight rollouts of 100 x 50000: 54 us against 104).
+template <int THREADS_, int PER_>
+struct LongShape {
+  static constexpr int THREADS = THREADS_, PER = PER_, STEP = THREADS_ * PER_;
+};
+constexpr int kLongSamples = 4;  // rollouts that one pass over the logits serves
 
-__global__ void __launch_bounds__(kLongThreads) policy_draw_long_kernel(PolicyDrawArgs a) {
-  __shared__ float red[kLongThreads / 64];
+template <class S>
+__global__ void __launch_bounds__(S::THREADS) policy_draw_long_kernel(PolicyDrawArgs a) {
+  constexpr int THREADS = S::THREADS;
+  constexpr int ALL = kLongSamples;
+  __shared__ float red_max[ALL + 1][THREADS / 64];
+  __shared__ float red_sum[1][THREADS / 64];
+  __shared__ float red_min[ALL][THREADS / 64];
   const int lane = threadIdx.x;
   for (long long r = blockIdx.x; r < a.count; r += gridDim.x) {
     const float* __restrict__ row = a.logits + r * a.K;
     Running w;
-    for (int s0 = 0; s0 < a.samples; s0 += kLongSamples) {
-      Best b[kLongSamples] = {Best(a.K), Best(a.K), Best(a.K), Best(a.K)};
-      for (int k0 = 0; k0 < a.K; k0 += kLongStep) {
-        float x[kLongPer];
-        row_read<kLongThreads, true>(row + k0, a.K - k0, lane, -INFINITY, x);
+    float lz = 0.f;
+    for (int s0 = 0; s0 < a.samples; s0 += ALL) {
+      Best b[ALL] = {Best(a.K), Best(a.K), Best(a.K), Best(a.K)};
+      for (int k0 = 0; k0 < a.K; k0 += S::STEP) {
+        float x[S::PER];
+        row_read<THREADS, true>(row + k0, a.K - k0, lane, -INFINITY, x);
 #pragma unroll
-        for (int s = 0; s < kLongSamples; ++s) {
+        for (int s = 0; s < ALL; ++s) {
           if (s0 + s >= a.samples) break;
-          float n[kLongPer];
-          row_read<kLongThreads, true>(a.noise + ((long long)(s0 + s) * a.count + r) * a.K + k0, a.K - k0, lane, 0.f, n);
+          float n[S::PER];
+          row_read<THREADS, true>(a.noise + ((long long)(s0 + s) * a.count + r) * a.K + k0, a.K - k0, lane, 0.f, n);
 #pragma unroll
-          for (int i = 0; i < kLongPer; ++i) b[s].take(x[i], n[i], k0 + quad_col<kLongThreads>(lane, i) + i % 4);
+          for (int i = 0; i < S::PER; ++i) b[s].take(x[i], n[i], k0 + quad_col<THREADS>(lane, i) + i % 4);
         }
         if (s0 == 0) w.add(x);
       }
-      if (s0 == 0) running_join<kLongThreads>(w, red);
+      float top[ALL + 1] = {b[0].score, b[1].score, b[2].score, b[3].score, w.m};
+      block_reduce<THREADS>(top, OpMax{}, red_max);
+      if (s0 == 0) {
+        w.rescale(top[ALL]);
+        float z[1] = {w.z};
+        block_reduce<THREADS>(z, OpSum{}, red_sum);
+        lz = logf(z[0]);
+      }
+      float first[ALL];
 #pragma unroll
-      for (int s = 0; s < kLongSamples; ++s) {
+      for (int s = 0; s < ALL; ++s) first[s] = b[s].score == top[s] ? (float)b[s].k : (float)a.K;
+      block_reduce<THREADS>(first, OpMin{}, red_min);
+#pragma unroll
+      for (int s = 0; s < ALL; ++s) {
         if (s0 + s >= a.samples) break;
-        const float top = block_reduce<kLongThreads>(b[s].score, OpMax{}, red);
-        const float first =
-            block_reduce<kLongThreads>(b[s].score == top ? (float)b[s].k : (float)a.K, OpMin{}, red);
-        best_write(a, (long long)(s0 + s) * a.count + r, b[s], top, first, lane == 0, row[0], w.m, logf(w.z));
+        best_write(a, (long long)(s0 + s) * a.count + r, b[s], top[s], first[s], lane == 0, row[0], w.m, lz);
       }
     }
   }
@@ -343,20 +361,27 @@ __global__ void __launch_bounds__(kPolicyThreads) policy_logp_rows_kernel(Policy
   }
 }
 
-__global__ void __launch_bounds__(kLongThreads) policy_logp_long_kernel(PolicyDrawArgs a) {
-  __shared__ float red[kLongThreads / 64];
+template <class S>
+__global__ void __launch_bounds__(S::THREADS) policy_logp_long_kernel(PolicyDrawArgs a) {
+  constexpr int THREADS = S::THREADS;
+  __shared__ float red_max[1][THREADS / 64];
+  __shared__ float red_sum[1][THREADS / 64];
   for (long long t = blockIdx.x; t < a.count; t += gridDim.x) {
     const long long r = tile_at<1, kRunLongRows>(t, a.count);
     const float* __restrict__ row = a.logits + r * a.K;
     Running w;
-    for (int k0 = 0; k0 < a.K; k0 += kLongStep) {
-      float x[kLongPer];
-      row_read<kLongThreads, true>(row + k0, a.K - k0, threadIdx.x, -INFINITY, x);
+    for (int k0 = 0; k0 < a.K; k0 += S::STEP) {
+      float x[S::PER];
+      row_read<THREADS, true>(row + k0, a.K - k0, threadIdx.x, -INFINITY, x);
       w.add(x);
     }
-    running_join<kLongThreads>(w, red);
-    const float lz = logf(w.z);
-    for (int s = threadIdx.x; s < a.samples; s += kLongThreads) {
+    float m[1] = {w.m};
+    block_reduce<THREADS>(m, OpMax{}, red_max);
+    w.rescale(m[0]);
+    float z[1] = {w.z};
+    block_reduce<THREADS>(z, OpSum{}, red_sum);
+    const float lz = logf(z[0]);
+    for (int s = threadIdx.x; s < a.samples; s += THREADS) {
       const long long o = (long long)s * a.count + r;
       a.logp[o] = logp_of(row, a.actions[o], a.K, w.m, lz);
     }
@@ -723,10 +748,12 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
 // then the first rollout that chose a level adds the slopes of all that did, in
 // their order, and writes that value again.  A thread's first choice and its
 // logit are read before the row.
+constexpr int kLongPer = 16;
 template <int THREADS, int HELD, int WAVES>
 __global__ void __launch_bounds__(THREADS, WAVES) policy_loss_long_kernel(PolicyLossArgs a) {
   constexpr int STEP = THREADS * kLongPer;
-  __shared__ float red[THREADS / 64];
+  __shared__ float red_max[1][THREADS / 64];
+  __shared__ float red_sum[2][THREADS / 64];
   __shared__ double redd[THREADS / 64];
   __shared__ float2 pairs[kMaxRollouts];
   __shared__ double terms[THREADS / 64][4];  // of each wave
@@ -762,11 +789,15 @@ __global__ void __launch_bounds__(THREADS, WAVES) policy_loss_long_kernel(Policy
       row_read<THREADS, true>(row + k0, K - k0, tid, -INFINITY, x);
       run.add(x);
     }
-    running_join<THREADS>(run, red);
+    float top[1] = {run.m};
+    block_reduce<THREADS>(top, OpMax{}, red_max);
+    run.rescale(top[0]);
+    float z[2] = {run.z, run.zd};
+    block_reduce<THREADS>(z, OpSum{}, red_sum);
     const float m = run.m;
-    const float inv_z = 1.f / run.z;
-    const float lz = logf(run.z);
-    const float h = lz - run.zd * inv_z;
+    const float inv_z = 1.f / z[0];
+    const float lz = logf(z[0]);
+    const float h = lz - z[1] * inv_z;
     bool near = false;
     Terms add;
 #pragma unroll 1
@@ -941,8 +972,13 @@ hipError_t launch_policy_draw(const PolicyDrawArgs& a, hipStream_t st) {
       },
       [&] {
         const dim3 grid((unsigned)std::min<long long>(a.count, 1 << 16));
-        if (a.noise) hipLaunchKernelGGL(policy_draw_long_kernel, grid, dim3(kLongThreads), 0, st, a);
-        else hipLaunchKernelGGL(policy_logp_long_kernel, grid, dim3(kLongThreads), 0, st, a);
+        auto go = [&](auto s) {
+          using S = decltype(s);
+          if (a.noise) hipLaunchKernelGGL((policy_draw_long_kernel<S>), grid, dim3(S::THREADS), 0, st, a);
+          else hipLaunchKernelGGL((policy_logp_long_kernel<S>), grid, dim3(S::THREADS), 0, st, a);
+        };
+        if (a.K <= 8192) go(LongShape<256, 8>{});
+        else go(LongShape<512, 16>{});
       });
   return hipGetLastError();
 }
