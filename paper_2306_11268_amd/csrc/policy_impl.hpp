@@ -742,15 +742,15 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
 
 // A workgroup per row of more than kPolicyRowMax levels.  HELD rounds of the
 // row (16 values a thread each) stay in registers between the sums and the
-// gradient, as many as still leave two workgroups to a CU, so that one loads
-// while the other computes; what a longer row has beyond them is read again
-// from the caches.  The gradient is written as if no level had been chosen;
+// gradient, as many as still leave 16 waves to a CU, of two workgroups or more,
+// so that one loads while another computes; what a longer row has beyond them is
+// read again from the caches.  The gradient is written as if no level had been chosen;
 // then the first rollout that chose a level adds the slopes of all that did, in
 // their order, and writes that value again.  A thread's first choice and its
 // logit are read before the row.
 constexpr int kLongPer = 16;
-template <int THREADS, int HELD, int WAVES>
-__global__ void __launch_bounds__(THREADS, WAVES) policy_loss_long_kernel(PolicyLossArgs a) {
+template <int THREADS, int HELD>
+__global__ void __launch_bounds__(THREADS, 4) policy_loss_long_kernel(PolicyLossArgs a) {
   constexpr int STEP = THREADS * kLongPer;
   __shared__ float red_max[1][THREADS / 64];
   __shared__ float red_sum[2][THREADS / 64];
@@ -1005,17 +1005,19 @@ hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) {
   };
   if (a.K > kPolicyRowMax) {
     grid = dim3((unsigned)std::min<long long>(a.count, kPolicyParts));
-    // (as many rounds held as the row has, up to four: 1500 rows of 65536 levels 210 -> 195 us from one to
-    // four, 6000 of 16384 179 -> 168 from one to two, but 205 with four, whose registers it does not fill; 1024
-    // threads, which hold such rows whole but fill a CU alone: 1600 of 40007 139 -> 149, 1500 of 65536 200 -> 200)
-    if (a.K <= 256 * kLongPer)
-      hipLaunchKernelGGL((policy_loss_long_kernel<256, 1, 6>), grid, dim3(256), 0, st, a);
-    else if (a.K <= 512 * kLongPer)
-      hipLaunchKernelGGL((policy_loss_long_kernel<512, 1, 6>), grid, dim3(512), 0, st, a);
-    else if (a.K <= 2 * 512 * kLongPer)
-      hipLaunchKernelGGL((policy_loss_long_kernel<512, 2, 4>), grid, dim3(512), 0, st, a);
-    else
-      hipLaunchKernelGGL((policy_loss_long_kernel<512, 4, 4>), grid, dim3(512), 0, st, a);
+    // (Rounds held: what 128 registers a lane take, the most of which are a row's values; with a fourth round, or
+    // with 80 registers for six waves on a SIMD, the compiler spills.  1600 rows of 40007 in bf16 111 us with four
+    // rounds, 97 with three; 1500 of 65536 194, 186.  Short rows in smaller workgroups, which wait for fewer waves:
+    // 16 rollouts of 20000 x 2500 148 -> 121 us with 128 threads and two rounds after 256 with one, of 10000 x 5000
+    // 134 -> 108 with 256 after 512.  1024 threads, which hold rows of 40007 whole but fill a CU alone: 139 -> 149.)
+    auto go = [&](auto threads, auto held) {
+      constexpr int THREADS = decltype(threads)::value;
+      hipLaunchKernelGGL((policy_loss_long_kernel<THREADS, decltype(held)::value>), grid, dim3(THREADS), 0, st, a);
+    };
+    using std::integral_constant;
+    if (a.K <= 2 * 128 * kLongPer) go(integral_constant<int, 128>{}, integral_constant<int, 2>{});
+    else if (a.K <= 2 * 256 * kLongPer) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    else go(integral_constant<int, 512>{}, integral_constant<int, 3>{});
   } else if (a.K % 4) {
     loss_rows_shape<true>(a.K, rows);
   } else {
