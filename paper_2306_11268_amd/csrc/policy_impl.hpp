@@ -141,17 +141,16 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 }
 
 // The tile that is worked as number t.  Workgroups go to the eight XCDs in turn,
-// so that the choices of neighbouring tiles, where they share cache lines, would
-// be fetched or completed once for each XCD's L2: every XCD takes runs of tiles
-// instead, ROWS rows long, as far as whole runs for all of them go.  For T >= 64
-// rows a tile's choices are lines of their own.  (Draws of four rollouts,
-// 200000 x 256: 180 -> 176 us, 50000 x 1000: 175 -> 164; log-probabilities of
-// eight, 612500 x 64: 43.0 -> 41.5, of sixteen, 200000 x 256: 44 -> 39.  The loss,
-// held by its arithmetic there and with longer tiles' rows apart for longer,
-// keeps the plain order: 97 us either way at 256 levels, 91 -> 97 at 2048.)
+// so that cache lines which the choices of neighbouring tiles share would be
+// fetched or completed once for each XCD's L2: every XCD takes runs of tiles
+// instead, ROWS rows long, as far as whole runs for all of them go.  (Draws of
+// four rollouts, 200000 x 256: 180 -> 175 us, 50000 x 1000: 175 -> 166;
+// log-probabilities of eight, 612500 x 64: 43.0 -> 41.4, of 16, 200000 x 256: 44 ->
+// 39, of 32, 612500 x 16: 43.0 -> 40.3.  The loss keeps the plain order: its
+// arithmetic has most of the time at few levels, 97 us either way at 256, and
+// 91 -> 97 at 2048.)
 template <int T, int ROWS>
 __device__ __forceinline__ long long tile_at(long long t, long long tiles) {
-  if constexpr (T >= 64) return t;
   constexpr int RUN = ROWS / T;
   const long long first = t / (8 * RUN) * (8 * RUN);
   if (first + 8 * RUN > tiles) return t;
