@@ -175,19 +175,18 @@ __device__ __forceinline__ float code_value(uint32_t c, float u) {
   // (2^(127 + LEAST) times u: 2 u 2^LEAST over float32's 2^-126)
   return __uint_as_float(c << 20) * __uint_as_float((254u + LEAST) << 23) * u;
 }
-// Code of the magnitude y in [0, 1) with 20 random bits: below 2^LEAST, adding
-// 2^LEAST puts the codes' distances into the same bits as above it.
-template <int LEAST>
-__device__ __forceinline__ uint32_t code_of(float y, uint32_t bits) {
-  const float least = __uint_as_float((127u + LEAST) << 23);
-  const bool small = y < least;
-  const uint32_t z = (__float_as_uint(small ? y + least : y) + bits) >> 20;
-  return z - (small ? ((126u + LEAST) << 3) + 8u : (126u + LEAST) << 3);
+// Code of the magnitude y (the value over two scales and times 2^(-126 - LEAST),
+// so that float32's subnormal numbers are the codes' too) with 20 random bits, in
+// the upper byte.
+__device__ __forceinline__ uint32_t code_of(float y, uint32_t bits) { return (__float_as_uint(y) + bits) << 4; }
+// The upper bytes of four words.
+__device__ __forceinline__ uint32_t upper_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(b, a, 0x0C0C0703u) | __builtin_amdgcn_perm(d, c, 0x07030C0Cu);
 }
 // Largest magnitude of the wave as bits (NaN and infinity the largest).
 __device__ __forceinline__ uint32_t wave_max_bits(uint32_t x) {
   auto dpp = [&](auto ctrl) {
-    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(ctrl)::value, 0xF, 0xF, false);
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xF, 0xF, true);
   };
   x = max(x, dpp(std::integral_constant<int, 0xB1>{}));
   x = max(x, dpp(std::integral_constant<int, 0x4E>{}));
@@ -202,16 +201,25 @@ __device__ __forceinline__ uint32_t wave_max_bits(uint32_t x) {
 // m and v after the step, p moved by them.
 __device__ __forceinline__ void adamw_values(const AdamwArgs& a, float clip, const float (&g4)[4], float (&m)[4],
                                              float (&v)[4], float (&p)[4]) {
+  float root[4];
+  uint32_t least = 0xFFFFFFFFu;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float g = mul_rn(g4[j], clip);  // (exact for clip = 1)
     m[j] = add_rn(mul_rn(m[j], a.b1), mul_rn(g, a.c1));
     v[j] = add_rn(mul_rn(v[j], a.b2), mul_rn(mul_rn(g, g), a.c2));
-    // (the root's instruction takes no subnormal numbers)
-    const bool tiny = v[j] < 0x1p-100f;
-    const float root = __builtin_amdgcn_sqrtf(tiny ? v[j] * 0x1p64f : v[j]) * (tiny ? 0x1p-32f : 1.f);
-    p[j] = p[j] * a.keep - a.rate * m[j] * __builtin_amdgcn_rcpf(root * a.root + a.eps);
+    root[j] = __builtin_amdgcn_sqrtf(v[j]);
+    least = min(least, __float_as_uint(v[j]) - 1u);
   }
+  // (the root's instruction takes no subnormal numbers, which are rare; zeros wrap around)
+  if (__any(least < 0x007FFFFFu)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (v[j] < 0x1p-100f) root[j] = __builtin_amdgcn_sqrtf(v[j] * 0x1p64f) * 0x1p-32f;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    p[j] = p[j] * a.keep - a.rate * m[j] * __builtin_amdgcn_rcpf(root[j] * a.root + a.eps);
 }
 
 template <bool BITS8, bool BF16, bool FULL>
@@ -220,12 +228,7 @@ __device__ __forceinline__ void adamw_chunk(const TensorEntry& t, const AdamwArg
   constexpr int AT_ONCE = BITS8 || RUNS < 2 ? RUNS : 2;  // runs in flight
   const int wave = threadIdx.x / 64;
   const int lane = threadIdx.x % 64;
-  float clip = 1.f;
-  if (a.norm) {
-    const float n = *a.norm;
-    if (!(fabsf(n) <= 3.402823466e38f)) return;
-    if (n > a.max_norm) clip = a.max_norm / n;
-  }
+  const float norm = a.norm ? *a.norm : 0.f;
 #pragma unroll
   for (int r0 = 0; r0 < RUNS; r0 += AT_ONCE) {
     float p[AT_ONCE][4], g[AT_ONCE][4];
@@ -251,6 +254,9 @@ __device__ __forceinline__ void adamw_chunk(const TensorEntry& t, const AdamwArg
         quad_f32<FULL>(t.v, i, t.count, v[r]);
       }
     }
+    // (behind the loads, so that they do not wait for it)
+    if (!(fabsf(norm) <= 3.402823466e38f)) return;
+    const float clip = norm > a.max_norm ? a.max_norm / norm : 1.f;
 #pragma unroll
     for (int r = 0; r < AT_ONCE; ++r) {
       const long long i = at(r);
@@ -274,28 +280,32 @@ __device__ __forceinline__ void adamw_chunk(const TensorEntry& t, const AdamwArg
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           top_m = max(top_m, __float_as_uint(fabsf(mm[j])));
-          top_v = max(top_v, __float_as_uint(vv[j]) & 0x7FFFFFFFu);
+          top_v = max(top_v, __float_as_uint(vv[j]));  // (a NaN's sign only makes it larger)
         }
         // exponents of the block, held where a scale and its inverse are normal numbers
         uint32_t em = wave_max_bits(top_m) >> 23;
         uint32_t ev = wave_max_bits(top_v) >> 23;
         em = max(em, 27u);
         ev = max(ev, 27u);
-        const float down_m = __uint_as_float((253u - min(em, 253u)) << 23);
-        const float down_v = __uint_as_float((253u - min(ev, 253u)) << 23);
         const uint32_t key = mix32(t.key + (uint32_t)((unsigned long long)i >> 32));
-        uint32_t wm = 0, wv = 0;
+        uint32_t zm[4], zv[4];
+        uint32_t least = 0xFFFFFFFFu;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t h = mix32((uint32_t)i + j + key);
-          uint32_t c = code_of<-14>(fabsf(mm[j]) * down_m, h & 0xFFFFFu);
-          c = c & 127u;
-          if (mm[j] < 0.f) c |= 128u;
-          wm |= c << (8 * j);
-          c = code_of<-30>(vv[j] * down_v, h >> 12) & 255u;
-          c = vv[j] > 0.f && c == 0u ? 1u : c;
-          wv |= c << (8 * j);
+          zm[j] = code_of(__builtin_ldexpf(fabsf(mm[j]), 14 - (int)em), h & 0xFFFFFu);
+          zv[j] = code_of(__builtin_ldexpf(vv[j], 30 - (int)ev), h >> 12);
+          least = min(least, zv[j]);
         }
+        if (__any(least < 1u << 24)) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (vv[j] > 0.f) zv[j] = max(zv[j], 1u << 24);
+        }
+        auto sign = [&](int j) { return __float_as_uint(mm[j] + 0.f); };  // (none of a negative zero)
+        uint32_t wm = upper_bytes(zm[0], zm[1], zm[2], zm[3]) |
+                      (upper_bytes(sign(0), sign(1), sign(2), sign(3)) & 0x80808080u);
+        uint32_t wv = upper_bytes(zv[0], zv[1], zv[2], zv[3]);
         if (em >= 253u) wm = 0;
         if (ev >= 253u) wv = 0;
         put_codes<FULL>(t.m, i, t.count, wm);
