@@ -1410,7 +1410,8 @@ int lr_policy_loss(const lr_policy* policy, const float* d_logits, const int32_t
   const lr::PolicyLossArgs a{d_logits, d_actions, d_old_logp, d_ref_logp, d_advantages, per_choice ? 1 : 0, samples,
                              levels, grad_type == LR_GRAD_BF16 ? 1 : 0, static_cast<long long>(count),
                              policy->clip_low, policy->clip_high, policy->kl_coef, policy->entropy_coef,
-                             policy->scale, d_grad_logits, d_loss, d_terms, static_cast<double*>(d_work)};
+                             policy->scale, 1.f - policy->clip_low, 1.f + policy->clip_high, d_grad_logits, d_loss,
+                             d_terms, static_cast<double*>(d_work)};
   return no_throw([&] { return run_timed("policy_loss", st, [&] { return lr::launch_policy_loss(a, st); }); });
 }
 

@@ -268,6 +268,7 @@ struct PolicyLossArgs {
   int bf16;  // type of grad
   long long count;
   float clip_low, clip_high, kl_coef, entropy_coef, scale;
+  float border_low, border_high;  // 1 - clip_low, 1 + clip_high
   void* grad;      // nullable
   float* loss;     // nullable
   float* terms;    // nullable, [4]

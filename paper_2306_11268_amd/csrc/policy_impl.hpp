@@ -27,7 +27,7 @@ constexpr int kPolicyCus = 256;  // of the MI355X
 template <int G, class Op>
 __device__ __forceinline__ float lanes_reduce(float x, Op op) {
   auto dpp = [&](auto ctrl) {
-    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, false));
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, true));
   };
   if constexpr (G >= 2) x = op(x, dpp(std::integral_constant<int, 0xB1>{}));   // quad_perm [1,0,3,2]
   if constexpr (G >= 4) x = op(x, dpp(std::integral_constant<int, 0x4E>{}));   // quad_perm [2,3,0,1]
@@ -393,15 +393,19 @@ struct Choice {
   int act;  // < 0: none
   float old, ref, adv;
 };
-// Rollout s, place o + k of the [samples][count] arrays (o in scalar registers
-// where the whole wave shares it).
-__device__ __forceinline__ Choice choice_read(const PolicyLossArgs& a, int s, long long o, unsigned k) {
-  Choice c;
-  c.act = (a.actions + o)[k];
-  c.old = (a.old_logp + o)[k];
-  c.ref = a.ref_logp ? (a.ref_logp + o)[k] : 0.f;
-  c.adv = a.per_choice ? (a.adv + o)[k] : a.adv[s];
-  return c;
+// Place o of the [samples][count] arrays, k bytes on; o_adv and k_adv of the
+// advantages, which may be [samples].  (o in scalar registers where a wave shares
+// it: a load then needs no address arithmetic.)
+template <class T>
+__device__ __forceinline__ T read_at(const T* p, long long o, unsigned k) {
+  return *reinterpret_cast<const T*>(reinterpret_cast<const char*>(p + o) + k);
+}
+__device__ __forceinline__ void choice_read(const PolicyLossArgs& a, long long o, unsigned k, long long o_adv,
+                                            unsigned k_adv, Choice& c) {
+  c.act = read_at(a.actions, o, k);
+  c.old = read_at(a.old_logp, o, k);
+  if (a.ref_logp) c.ref = read_at(a.ref_logp, o, k);
+  c.adv = read_at(a.adv, o_adv, k_adv);
 }
 // What the choices of one thread add to the loss's terms.
 struct Terms {
@@ -421,7 +425,7 @@ __device__ __forceinline__ void terms_add(const Terms& t, double* sum) {
   }
 }
 // A choice under the present logits.  d: its level's logit minus the row's
-// maximum, NaN for a level out of range.
+// maximum.
 struct Ratio {
   float logp, ratio, border;
   float over;  // > 0: on the clipped side
@@ -429,31 +433,29 @@ struct Ratio {
     logp = d - lz;
     ratio = exp_fast(logp - c.old);
     const bool up = c.adv >= 0.f;
-    border = up ? 1.f + a.clip_high : 1.f - a.clip_low;
-    over = up ? ratio - border : border - ratio;
+    border = up ? a.border_high : a.border_low;
+    over = ratio - border;
+    over = up ? over : -over;
   }
   // So near to the border that float32 may put it on the wrong side: the errors
   // of the log-probability (of d, the sum of exponentials and its logarithm)
   // reach over it.  There the log-probability is within 90 of old, and |d|
-  // within lz of the log-probability.
-  __device__ __forceinline__ bool open(const Choice& c, float lz) const {
-    return fabsf(over) <= border * (3.6e-7f * (fabsf(c.old) + lz) + 2.6e-5f);
+  // within lz of the log-probability.  row: of open_row.
+  __device__ __forceinline__ bool open(const PolicyLossArgs& a, const Choice& c, float row) const {
+    return fabsf(over) <= fmaf(fabsf(c.old), 3.6e-7f * a.border_high, row);
   }
+  // A level out of range.
+  __device__ __forceinline__ void spoil() { logp = ratio = over = __builtin_nanf(""); }
 };
-// dl/dlogp (times scale) of a choice, its terms added to t; h: the row's
-// entropy.  Without branches: a place without a choice (whose numbers may be
-// anything) is left out at the end.
-__device__ __forceinline__ float choice_slope(const PolicyLossArgs& a, const Choice& c, const Ratio& r, float h,
-                                              Terms& t) {
-  const bool made = c.act >= 0;
-  const bool real = c.act < a.K;
+__device__ __forceinline__ float open_row(const PolicyLossArgs& a, float lz) {
+  return a.border_high * (3.6e-7f * lz + 2.6e-5f);
+}
+// dl/dlogp (times scale) of a choice that was made; its gain and KL added to t.
+__device__ __forceinline__ float choice_slope(const PolicyLossArgs& a, const Choice& c, const Ratio& r, Terms& t) {
   const bool cut = r.over > 0.f;
   const float g = r.ratio * c.adv;
-  const float gain = cut ? r.border * c.adv : g;
+  t.gain += cut ? r.border * c.adv : g;
   float slope = cut ? 0.f : -g;
-  t.gain += made ? gain : 0.f;
-  t.entropy += made ? (real ? h : __builtin_nanf("")) : 0.f;
-  t.cut += made ? (cut ? 1.f : real ? 0.f : __builtin_nanf("")) : 0.f;
   if (a.ref_logp) {
     // e^k - 1 - k: by its series where the difference would cancel
     const float k = c.ref - r.logp;
@@ -466,11 +468,14 @@ __device__ __forceinline__ float choice_slope(const PolicyLossArgs& a, const Cho
     q = q * k + 1.f / 24;
     q = q * k + 1.f / 6;
     q = (q * k + 0.5f) * k * k;
-    if (__any(!(fabsf(k) < 1.f)) && !(fabsf(k) < 1.f)) q = (exp_fast(k) - 1.f) - k;
-    t.kl += made ? q : 0.f;
+    if (__builtin_amdgcn_ballot_w64(!(fabsf(k) < 1.f))) {
+      asm volatile("");  // (a branch, or every wave forms both)
+      if (!(fabsf(k) < 1.f)) q = (exp_fast(k) - 1.f) - k;
+    }
+    t.kl += q;
     if (a.kl_coef != 0.f) slope -= a.kl_coef * (k + q);  // (not 0 times infinity)
   }
-  return made ? slope * a.scale : 0.f;
+  return slope * a.scale;
 }
 // e^x for |x| < 700 to about 1e-13: 2^k times the series of the rest, at most
 // ln(2) / 2 (0.35^12 / 12! < 1e-14).  Rolled, its coefficients in memory: the
@@ -588,13 +593,24 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
     const int mine_row = tid % T;  // whose choices this thread takes, STEP rollouts apart
     int part = tid / T;
     if constexpr (T % 64 == 0) part = __builtin_amdgcn_readfirstlane(part);
+    const bool live = r0 + mine_row < a.count;
     long long at = part * a.count + r0;
-    auto fetch = [&](int s, long long o) {
-      Choice c{-1, 0.f, 0.f, 0.f};
-      if (s < a.samples && part < STEP && r0 + mine_row < a.count) c = choice_read(a, s, o, mine_row);
-      return c;
+    long long adv_at = a.per_choice ? at : part;
+    const long long adv_step = a.per_choice ? STEP * a.count : STEP;
+    // The thread's next choice is read into c, or marked as none (its other numbers are then any).
+    auto fetch = [&](int s, Choice& c) {
+      c.act = -1;
+      if (s < a.samples && part < STEP && live) {
+        unsigned k = 4 * mine_row;
+        if constexpr (T % 64 == 0) {
+          asm volatile("" : "+v"(k));  // (or the arrays' places of this thread take eight registers)
+          k &= 4 * T - 1;
+        }
+        choice_read(a, at, k, adv_at, a.per_choice ? k : 0u, c);
+      }
     };
-    Choice next = fetch(part, at);
+    Choice next{-1, 0.f, 0.f, 0.f};
+    fetch(part, next);
     float d[N];
     row_read<G, TAIL>(a.logits + (r0 + row) * K, ok ? K : 0, lane, -INFINITY, d);
     float m = d[0];
@@ -635,34 +651,53 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
     Terms add;
     __syncthreads();
     const float2 row_stat = stat[mine_row];
+    const float row_open = open_row(a, row_stat.x);
     const float row_m = stat_m[mine_row];
     const float* row_d = lds + mine_row * stride;
     float* row_add = lds + (DIRECT ? (1 + part) * table : 0) + mine_row * stride;
+    float chosen = 0.f;  // choices of this thread
+    unsigned cuts = 0;   // of this wave, on the clipped side
     // The thread's next choice.  (A wave's lanes go through it together: those without one have act = -1.)
     auto choose = [&](int s, bool near_lds) {
       const Choice c = next;
       at += STEP * a.count;
-      next = fetch(s + STEP, at);
-      const bool real = (unsigned)c.act < (unsigned)K;
+      adv_at += adv_step;
+      fetch(s + STEP, next);
+      const int level = min(max(c.act, 0), K - 1);
       float dx;
-      if (near_lds) dx = row_d[real ? c.act : 0];
-      else dx = floor_d(a.logits[real ? (r0 + mine_row) * K + c.act : 0] - row_m);
-      Ratio ratio(a, c, c.act < K ? dx : __builtin_nanf(""), row_stat.x);
+      if (near_lds) dx = row_d[level];
+      else dx = floor_d(a.logits[live ? (r0 + mine_row) * K + level : 0] - row_m);
+      Ratio ratio(a, c, dx, row_stat.x);
+      const bool is_made = c.act >= 0;
+      if (__builtin_amdgcn_ballot_w64(c.act >= K)) {
+        asm volatile("");
+        if (c.act >= K) {
+          ratio.spoil();
+          add.entropy = add.cut = __builtin_nanf("");
+        }
+      }
       // undecided choices: the wave forms their rows' sums again, in 64 bits
-      for (unsigned long long open = __ballot(real && ratio.open(c, row_stat.x)); open; open &= open - 1) {
+      for (unsigned long long open = __builtin_amdgcn_ballot_w64(is_made && ratio.open(a, c, row_open)); open;
+           open &= open - 1) {
         const int who = __builtin_ctzll(open);
         const float* p = a.logits + (r0 + __shfl(mine_row, who, 64)) * K;
         const double zr = wave_sum_exp_d(p, K, __shfl(row_m, who, 64));
-        if ((int)(threadIdx.x & 63) == who) ratio.over = over_d(a, c, p[c.act], row_m, zr);
+        if ((int)(threadIdx.x & 63) == who) ratio.over = over_d(a, c, p[level], row_m, zr);
       }
-      return make_float2(__int_as_float(c.act), choice_slope(a, c, ratio, row_stat.y, add));
+      cuts += __popcll(__builtin_amdgcn_ballot_w64(is_made && ratio.over > 0.f));
+      float slope = 0.f;
+      if (is_made) {
+        chosen += 1.f;
+        slope = choice_slope(a, c, ratio, add);
+      }
+      return make_float2(__int_as_float(DIRECT ? (is_made ? level : -1) : c.act), slope);
     };
     auto collect = [&](float2 c) {
       const int act = __float_as_int(c.x);
       if (act >= 0) {
         made += 1.f;
         slopes += c.y;
-        if (act >= K) return;
+        if (!DIRECT && act >= K) return;
         // (a place of this lane alone.  Where it has all of a row's rollouts, the atomic lets it go on without
         // the sum; where every lane adds, the atomics' rate holds the pass: 612500 x 16, 32 rollouts 132 -> 82 us)
         if (DIRECT) row_add[act] += c.y;
@@ -702,6 +737,8 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
         if (s1 < a.samples) __syncthreads();
       }
     }
+    if (chosen > 0.f) add.entropy += chosen * row_stat.y;
+    if (tid % 64 == 0) add.cut += (float)cuts;
     terms_add(add, terms[tid / 64]);
     __syncthreads();
     if (a.grad) {
@@ -765,9 +802,17 @@ __global__ void __launch_bounds__(THREADS, 4) policy_loss_long_kernel(PolicyLoss
     asm volatile("" : "+s"(K));
     const float* __restrict__ row = a.logits + r * K;
     auto fetch = [&](int s, float& x) {
-      const Choice c = choice_read(a, s, (long long)s * a.count + r, 0u);
+      Choice c{-1, 0.f, 0.f, 0.f};
+      const long long at = (long long)s * a.count + r;
+      choice_read(a, at, 0u, a.per_choice ? at : s, 0u, c);
       x = (unsigned)c.act < (unsigned)K ? row[c.act] : 0.f;
       return c;
+    };
+    auto slope_of = [&](const Choice& c, const Ratio& ratio, float h, Terms& t) {
+      if (c.act < 0) return 0.f;
+      t.entropy += h;
+      t.cut += ratio.over > 0.f ? 1.f : 0.f;
+      return choice_slope(a, c, ratio, t);
     };
     Choice c0{-1, 0.f, 0.f, 0.f};
     float x0 = 0.f;
@@ -805,11 +850,15 @@ __global__ void __launch_bounds__(THREADS, 4) policy_loss_long_kernel(PolicyLoss
       float x = x0;
       if (s != tid) c = fetch(s, x);
       const bool real = (unsigned)c.act < (unsigned)K;
-      const Ratio ratio(a, c, real ? floor_d(x - m) : __builtin_nanf(""), lz);
-      const bool here = real && ratio.open(c, lz);
+      Ratio ratio(a, c, floor_d(x - m), lz);
+      if (c.act >= K) {
+        ratio.spoil();
+        add.entropy = add.cut = __builtin_nanf("");
+      }
+      const bool here = real && ratio.open(a, c, open_row(a, lz));
       near |= here;
       // (an undecided choice is left to the second pass)
-      const float g = here ? 0.f : choice_slope(a, c, ratio, h, add);
+      const float g = here ? 0.f : slope_of(c, ratio, h, add);
       pairs[s] = make_float2(__int_as_float(here ? -2 : (c.act < 0 ? -1 : c.act)), g);
     }
     if (__syncthreads_or(near)) {
@@ -821,7 +870,7 @@ __global__ void __launch_bounds__(THREADS, 4) policy_loss_long_kernel(PolicyLoss
         const Choice c = fetch(s, x);
         Ratio ratio(a, c, x - m, lz);
         ratio.over = over_d(a, c, x, m, zr);
-        pairs[s] = make_float2(__int_as_float(c.act), choice_slope(a, c, ratio, h, add));
+        pairs[s] = make_float2(__int_as_float(c.act), slope_of(c, ratio, h, add));
       }
       __syncthreads();
     }
