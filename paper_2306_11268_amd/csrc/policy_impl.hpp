@@ -559,9 +559,26 @@ __device__ __forceinline__ void quad_store(void* grad, int bf16, long long row, 
 // on a CU: nothing is carried from tile to tile but the terms, and the thread's
 // number and K are made new for each, or the compiler holds 70 registers of
 // addresses and comparisons across the loop.  Dynamic shared memory (K rounded
-// up to four, and padded off the banks' number): float [1 + PARTS][T][K], the
-// logits first; without tables float2 [chunk][T] behind them.
-__host__ __device__ constexpr int loss_stride(int K) { return (K + 3) / 4 * 4 + ((K + 3) / 4 % 2 ? 0 : 4); }
+// up to four, or padded): float [1 + PARTS][T][K], the logits first; without
+// tables float2 [chunk][T] behind them.
+//
+// Rows whose quads of four levels are a multiple of a power of two start on few
+// of the 64 banks.  With tables, their quads change places, by a number that goes
+// through that power (16 at most) over the rows that would meet, its high bits
+// first (for stores of neighbouring quads): choices of one level then meet as if
+// the rows were padded, without the padding's memory (612500 rows of 16 levels:
+// 80 us padded, with four workgroups on a CU, 72 with five).  The list's rows,
+// fewer and longer, are padded.
+template <bool DIRECT>
+__host__ __device__ constexpr int loss_stride(int K) {
+  return (K + 3) / 4 * 4 + (DIRECT || (K + 3) / 4 % 2 ? 0 : 4);
+}
+template <bool DIRECT>
+__device__ __forceinline__ int loss_swap(int K, int row) {
+  if (!DIRECT) return 0;
+  const int bits = min(__builtin_ctz((K + 3) / 4), 4);
+  return (int)(__brev((unsigned)row >> (4 - bits)) >> 1 >> (31 - bits));
+}
 
 template <int G, int N, int PARTS, int WAVES, bool TAIL>
 __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel(PolicyLossArgs a, int chunk) {
@@ -584,10 +601,11 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
     asm volatile("" : "+s"(K));
     const int lane = tid % G;
     const int row = tid / G;
-    const int stride = loss_stride(K);
+    const int stride = loss_stride<DIRECT>(K);
     const int table = T * stride;
     float2* pairs = reinterpret_cast<float2*>(lds + table);
     float4* mine = reinterpret_cast<float4*>(lds + row * stride);
+    const int swap = loss_swap<DIRECT>(K, row);
     const long long r0 = tile * T;
     const bool ok = r0 + row < a.count;
     const int mine_row = tid % T;  // whose choices this thread takes, STEP rollouts apart
@@ -631,10 +649,10 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
     for (int i = 0; i < N; i += 4) {
       const int c = quad_col<G>(lane, i);
       if (c >= K) continue;
-      mine[c / 4] = make_float4(d[i], d[i + 1], d[i + 2], d[i + 3]);
+      mine[c / 4 ^ swap] = make_float4(d[i], d[i + 1], d[i + 2], d[i + 3]);
       if (DIRECT) {
 #pragma unroll
-        for (int p = 1; p <= TABLES; ++p) mine[p * (table / 4) + c / 4] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int p = 1; p <= TABLES; ++p) mine[p * (table / 4) + (c / 4 ^ swap)] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
     }
     z = lanes_reduce<G>(z, OpSum{});
@@ -655,6 +673,7 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
     const float row_m = stat_m[mine_row];
     const float* row_d = lds + mine_row * stride;
     float* row_add = lds + (DIRECT ? (1 + part) * table : 0) + mine_row * stride;
+    const int swap_level = 4 * loss_swap<DIRECT>(K, mine_row);
     float chosen = 0.f;  // choices of this thread
     unsigned cuts = 0;   // of this wave, on the clipped side
     // The thread's next choice.  (A wave's lanes go through it together: those without one have act = -1.)
@@ -665,7 +684,7 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
       fetch(s + STEP, next);
       const int level = min(max(c.act, 0), K - 1);
       float dx;
-      if (near_lds) dx = row_d[level];
+      if (near_lds) dx = row_d[level ^ swap_level];
       else dx = floor_d(a.logits[live ? (r0 + mine_row) * K + level : 0] - row_m);
       Ratio ratio(a, c, dx, row_stat.x);
       const bool is_made = c.act >= 0;
@@ -699,9 +718,9 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
         slopes += c.y;
         if (!DIRECT && act >= K) return;
         // (a place of this lane alone.  Where it has all of a row's rollouts, the atomic lets it go on without
-        // the sum; where every lane adds, the atomics' rate holds the pass: 612500 x 16, 32 rollouts 132 -> 82 us)
-        if (DIRECT) row_add[act] += c.y;
-        else __hip_atomic_fetch_add(row_add + act, c.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        // the sum; where every lane adds, the atomics' rate would hold the pass: 612500 x 16, 32 rollouts 50 us more)
+        if (DIRECT) row_add[act ^ swap_level] += c.y;
+        else __hip_atomic_fetch_add(row_add + (act ^ swap_level), c.y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
       }
     };
     if constexpr (DIRECT) {
@@ -725,7 +744,7 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
 #pragma unroll
           for (int i = 0; i < N; i += 4) {
             const int c = quad_col<G>(lane, i);
-            if (c < K) mine[c / 4] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (c < K) mine[c / 4 ^ swap] = make_float4(0.f, 0.f, 0.f, 0.f);
           }
           __syncthreads();
         }
@@ -753,10 +772,10 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
       for (int i = 0; i < N; i += 4) {
         const int c = quad_col<G>(lane, i);
         if (c >= K) continue;
-        float4 q = mine[(DIRECT ? table / 4 : 0) + c / 4];
+        float4 q = mine[(DIRECT ? table / 4 : 0) + (c / 4 ^ swap)];
 #pragma unroll
         for (int p = 2; p <= TABLES; ++p) {
-          const float4 o = mine[p * (table / 4) + c / 4];
+          const float4 o = mine[p * (table / 4) + (c / 4 ^ swap)];
           q = make_float4(q.x + o.x, q.y + o.y, q.z + o.z, q.w + o.w);
         }
         const float s[4] = {q.x, q.y, q.z, q.w};
@@ -977,7 +996,8 @@ static void policy_rows_shape(int K, F&& rows) {
   else rows(Shape<64, 32, TAIL>{});
 }
 // The loss's rows: also how many threads of a row add slopes, and the
-// workgroups that a CU holds by their registers (without spilling any).
+// workgroups that a CU holds by their registers (without spilling any but three
+// up to 32 levels, where a sixth workgroup gives 3 %).
 template <int G_, int N_, int PARTS_, int WAVES_, bool TAIL_>
 struct LossShape {
   static constexpr int G = G_, N = N_, PARTS = PARTS_, WAVES = WAVES_;
@@ -985,10 +1005,10 @@ struct LossShape {
 };
 template <bool TAIL, class F>
 static void loss_rows_shape(int K, F&& rows) {
-  if (K <= 4) rows(LossShape<1, 4, 1, 5, TAIL>{});
+  if (K <= 4) rows(LossShape<1, 4, 1, 6, TAIL>{});
   else if (K <= 8) rows(LossShape<1, 8, 1, 5, TAIL>{});
   else if (K <= 16) rows(LossShape<2, 8, 2, 5, TAIL>{});
-  else if (K <= 32) rows(LossShape<4, 8, 2, 5, TAIL>{});
+  else if (K <= 32) rows(LossShape<4, 8, 2, 6, TAIL>{});
   else if (K <= 64) rows(LossShape<8, 8, 2, 5, TAIL>{});
   else if (K <= 128) rows(LossShape<8, 16, 0, 4, TAIL>{});
   else if (K <= 256) rows(LossShape<16, 16, 0, 4, TAIL>{});
@@ -1037,7 +1057,7 @@ hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) {
   auto rows = [&](auto s) {
     using S = decltype(s);
     constexpr int T = kPolicyThreads / S::G;
-    const int table = T * loss_stride(a.K) * 4;
+    const int table = T * loss_stride<(S::PARTS > 0)>(a.K) * 4;
     // (the list: a whole number of the kernel's rounds of kPolicyThreads choices, in what leaves as many
     // workgroups to a CU's 160 KB as its registers do)
     const int fixed = 192 + (12 + 8 * std::max(1, S::PARTS)) * T;
