@@ -8,10 +8,11 @@
 // its largest exponents are found in the wave.  Nothing is read or written
 // twice: 28 bytes a value with float32 moments and gradients, 14 with 8-bit
 // moments and bf16 gradients.  Memory bounds them (a large copy: 5.0 TB/s):
-// 165 M values with 8-bit moments 440 us (5.2 TB/s), their moments written out
-// 262 us (6.3 TB/s, mostly stores), the norm of as many bf16 gradients 60 us
+// 165 M values with 8-bit moments 415 us (5.6 TB/s), their moments written out
+// 264 us (6.3 TB/s, mostly stores), the norm of as many bf16 gradients 60 us
 // (5.5 TB/s); 200 tensors of together 22.2 M values with float32 moments, three
-// launches, 131 us (4.7 TB/s).
+// launches, 131 us (4.7 TB/s).  With 8-bit moments the vector instructions come
+// next (66 a value, 308 us at the peak rate): 93 of them took 440 us.
 #pragma once
 
 #include "kernels.hpp"

@@ -280,9 +280,8 @@ hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st);
 // values (a kernel argument: a launch may be captured, and hundreds of tensors
 // take a few launches).  chunk0: the tensor's first chunk of the launch's, which
 // are fewer than 2^31.  Chunks as measured: the norm of 165 M bf16 values 63,
-// 67, 83 us with 4096, 2048, 1024; a step of 200 tensors 164, 143 us and one with
-// 8-bit moments over 165 M values, with their decoding, 722, 697 us with 4096,
-// 1024.
+// 67, 83 us with 4096, 2048, 1024; a step of 200 tensors 146, 133, 131 us and one
+// with 8-bit moments over 165 M values, with their decoding, 716, 720, 682 us.
 constexpr int kNormChunk = 4096;
 constexpr int kStepChunk = 1024;  // of lr_adamw_update and lr_adamw_moments
 constexpr int kStateBlock = 256;  // values that share the scales of 8-bit moments

@@ -146,9 +146,9 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 // instead, ROWS rows long, as far as whole runs for all of them go.  (Draws of
 // four rollouts, 200000 x 256: 180 -> 175 us, 50000 x 1000: 175 -> 166;
 // log-probabilities of eight, 612500 x 64: 43.0 -> 41.4, of 16, 200000 x 256: 44 ->
-// 39, of 32, 612500 x 16: 43.0 -> 40.3.  The loss keeps the plain order: its
-// arithmetic has most of the time at few levels, 97 us either way at 256, and
-// 91 -> 97 at 2048.)
+// 39, of 32, 612500 x 16: 43.0 -> 40.3.  The loss keeps the plain order, though it
+// fetches such lines more than once: 97 us either way at 256 levels and 71 at 16,
+// 69 -> 73 at 32, 91 -> 95 at 2048.)
 template <int T, int ROWS>
 __device__ __forceinline__ long long tile_at(long long t, long long tiles) {
   constexpr int RUN = ROWS / T;
@@ -441,15 +441,13 @@ struct Ratio {
   // of the log-probability (of d, the sum of exponentials and its logarithm)
   // reach over it.  There the log-probability is within 90 of old, and |d|
   // within lz of the log-probability.  row: of open_row.
-  __device__ __forceinline__ bool open(const PolicyLossArgs& a, const Choice& c, float row) const {
-    return fabsf(over) <= fmaf(fabsf(c.old), 3.6e-7f * a.border_high, row);
+  __device__ __forceinline__ bool open(const Choice& c, float row) const {
+    return fabsf(over) <= border * fmaf(fabsf(c.old), 3.6e-7f, row);
   }
   // A level out of range.
   __device__ __forceinline__ void spoil() { logp = ratio = over = __builtin_nanf(""); }
 };
-__device__ __forceinline__ float open_row(const PolicyLossArgs& a, float lz) {
-  return a.border_high * (3.6e-7f * lz + 2.6e-5f);
-}
+__device__ __forceinline__ float open_row(float lz) { return 3.6e-7f * lz + 2.6e-5f; }
 // dl/dlogp (times scale) of a choice that was made; its gain and KL added to t.
 __device__ __forceinline__ float choice_slope(const PolicyLossArgs& a, const Choice& c, const Ratio& r, Terms& t) {
   const bool cut = r.over > 0.f;
@@ -669,7 +667,7 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
     Terms add;
     __syncthreads();
     const float2 row_stat = stat[mine_row];
-    const float row_open = open_row(a, row_stat.x);
+    const float row_open = open_row(row_stat.x);
     const float row_m = stat_m[mine_row];
     const float* row_d = lds + mine_row * stride;
     float* row_add = lds + (DIRECT ? (1 + part) * table : 0) + mine_row * stride;
@@ -696,7 +694,7 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
         }
       }
       // undecided choices: the wave forms their rows' sums again, in 64 bits
-      for (unsigned long long open = __builtin_amdgcn_ballot_w64(is_made && ratio.open(a, c, row_open)); open;
+      for (unsigned long long open = __builtin_amdgcn_ballot_w64(is_made && ratio.open(c, row_open)); open;
            open &= open - 1) {
         const int who = __builtin_ctzll(open);
         const float* p = a.logits + (r0 + __shfl(mine_row, who, 64)) * K;
@@ -874,7 +872,7 @@ __global__ void __launch_bounds__(THREADS, 4) policy_loss_long_kernel(PolicyLoss
         ratio.spoil();
         add.entropy = add.cut = __builtin_nanf("");
       }
-      const bool here = real && ratio.open(a, c, open_row(a, lz));
+      const bool here = real && ratio.open(c, open_row(lz));
       near |= here;
       // (an undecided choice is left to the second pass)
       const float g = here ? 0.f : slope_of(c, ratio, h, add);

@@ -236,6 +236,22 @@ def test_ratios_next_to_the_clip_borders(lrb, k):
     assert int(round(float(terms[3]))) == int((over & clear).sum())
 
 
+@pytest.mark.parametrize("k", (3, 16, 40, 256, 3000))
+@pytest.mark.parametrize("low,high", [(1.0, 1e6), (1.0, 0.0), (0.0, 0.0), (0.0, 3e38)])
+def test_clips_at_their_limits_and_far_references(lrb, k, low, high):
+    """Ratios of e^-3 to e^3, none within e^0.05 of one; references e^-4 to e^4 away, where e^d - d - 1 is formed as it
+    stands (off by at most 1.7 times the error of d, which is below 150 u)."""
+    g = rng(15, k)
+    x, a, _, adv, _ = loss_inputs(g, 33, k, 5, True, True)
+    lp = ot.policy_logp(x, a)
+    away = g.uniform(0.05, 3.0, a.shape) * np.where(g.uniform(size=a.shape) < 0.5, 1, -1)
+    old = (lp - away).astype(np.float32)
+    ref = (lp + g.uniform(-4.0, 4.0, a.shape)).astype(np.float32)
+    a[2, 5] = a[0, 0] = -1
+    check_loss(lrb, x, a, old, adv, ref, clip_low=low, clip_high=high, kl_coef=0.03)
+    check_loss(lrb, x, a, old, adv, None, clip_low=low, clip_high=high, entropy_coef=0.0)
+
+
 def test_outputs_on_their_own_and_together_are_the_same(lrb):
     x, a, old, adv, ref = (dev(t) for t in loss_inputs(rng(9), 300, 64, 4, False, True))
     loss, terms, grad = lrb.lr_policy_loss(x, a, old, adv, ref_logp=ref, **KW)
