@@ -19,6 +19,8 @@ namespace lr {
 constexpr int kPolicyRowMax = 2048;
 constexpr int kPolicyThreads = 256;
 constexpr int kPolicyCus = 256;  // of the MI355X
+constexpr int kLdsUnit = 1280;   // bytes that shared memory is given out by
+constexpr int kLdsUnits = 128;   // of a CU
 
 // ---- reductions on the vector ALU (no shared memory) -----------------------
 // Lanes 1, 2, 4, 8 apart through DPP (where pairs, quads, ... already agree, the
@@ -994,8 +996,11 @@ static void policy_rows_shape(int K, F&& rows) {
   else rows(Shape<64, 32, TAIL>{});
 }
 // The loss's rows: also how many threads of a row add slopes, and the
-// workgroups that a CU holds by their registers (without spilling any but three
-// up to 32 levels, where a sixth workgroup gives 3 %).
+// workgroups that a CU holds by their registers (without spilling any but two up
+// to 32 levels, where a sixth workgroup gives 3 %).  With tables every thread of
+// a workgroup takes choices up to 24 levels, and half of them above, so rows share
+// few lanes: 32 rollouts of 612500 x 24 105 us with four lanes a row, 88 with two;
+// 16 of 400000 x 40 66 with eight, 51 with four, of 400000 x 64 82, 80.
 template <int G_, int N_, int PARTS_, int WAVES_, bool TAIL_>
 struct LossShape {
   static constexpr int G = G_, N = N_, PARTS = PARTS_, WAVES = WAVES_;
@@ -1006,8 +1011,10 @@ static void loss_rows_shape(int K, F&& rows) {
   if (K <= 4) rows(LossShape<1, 4, 1, 6, TAIL>{});
   else if (K <= 8) rows(LossShape<1, 8, 1, 5, TAIL>{});
   else if (K <= 16) rows(LossShape<2, 8, 2, 5, TAIL>{});
+  else if (K <= 24) rows(LossShape<2, 12, 2, 5, TAIL>{});
   else if (K <= 32) rows(LossShape<4, 8, 2, 6, TAIL>{});
-  else if (K <= 64) rows(LossShape<8, 8, 2, 5, TAIL>{});
+  else if (K <= 48) rows(LossShape<4, 12, 2, 5, TAIL>{});
+  else if (K <= 64) rows(LossShape<4, 16, 2, 4, TAIL>{});
   else if (K <= 128) rows(LossShape<8, 16, 0, 4, TAIL>{});
   else if (K <= 256) rows(LossShape<16, 16, 0, 4, TAIL>{});
   else if (K <= 512) rows(LossShape<32, 16, 0, 4, TAIL>{});
@@ -1058,14 +1065,16 @@ hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) {
     const int table = T * loss_stride<(S::PARTS > 0)>(a.K) * 4;
     // (the list: a whole number of the kernel's rounds of kPolicyThreads choices, in what leaves as many
     // workgroups to a CU's 160 KB as its registers do)
-    const int fixed = 192 + (12 + 8 * std::max(1, S::PARTS)) * T;
-    const int fit = (163840 / S::WAVES - fixed - table) / (8 * kPolicyThreads);
+    const int fixed = 128 + (12 + 8 * std::max(1, S::PARTS)) * T;
+    const int fit = (kLdsUnits / S::WAVES * kLdsUnit - fixed - table) / (8 * kPolicyThreads);
     const int rounds = (a.samples + S::G - 1) / S::G;
     const int chunk = std::max(1, std::min(rounds, std::min(fit, 8))) * S::G;
-    const size_t lds = S::PARTS ? (size_t)table * (1 + S::PARTS) : table + (size_t)chunk * T * 8;
-    // as many workgroups as run at once: a second, smaller round of them would leave CUs idle
+    const int lds = S::PARTS ? table * (1 + S::PARTS) : table + chunk * T * 8;
+    // as many workgroups as run at once: a second, smaller round of them would leave CUs idle (400000 x 40, 16
+    // rollouts: 64 us with one workgroup for each CU more than its shared memory takes, 51 without)
     static_assert(kPolicyCus * S::WAVES <= kPolicyParts, "partial sums");
-    grid = policy_grid<S::G>(a.count, kPolicyCus * std::min<long long>(S::WAVES, 163840 / (lds + fixed)));
+    const int units = (lds + fixed + kLdsUnit - 1) / kLdsUnit;
+    grid = policy_grid<S::G>(a.count, kPolicyCus * std::min(S::WAVES, kLdsUnits / units));
     hipLaunchKernelGGL((policy_loss_rows_kernel<S::G, S::N, S::PARTS, S::WAVES, S::TAIL>), grid, dim3(kPolicyThreads),
                        lds, st, a, chunk);
   };

@@ -409,3 +409,11 @@ def test_levels_barred_by_very_low_scores(lrb, k, low):
     got, glp, _ = lrb.lr_policy_draw(dev(x), dev(noise))
     assert np.array_equal(host(got), ot.policy_draw(x, noise))
     check_logp(x, host(got), host(glp))
+
+
+@pytest.mark.parametrize("k,rows", [(12, 330001), (20, 200003), (24, 220001), (25, 190001), (40, 130001), (47, 90001),
+                                    (48, 110001), (49, 90001), (63, 90001)])
+def test_level_counts_between_the_powers_of_two(lrb, k, rows):
+    test_loss_and_gradient(lrb, k)
+    test_missing_choices_barred_levels_and_empty_rows(lrb, k)
+    test_more_tiles_than_workgroups(lrb, k, rows)
