@@ -457,7 +457,8 @@ __device__ __forceinline__ float choice_slope(const PolicyLossArgs& a, const Cho
   t.gain += cut ? r.border * c.adv : g;
   float slope = cut ? 0.f : -g;
   if (a.ref_logp) {
-    // e^k - 1 - k: by its series where the difference would cancel
+    // q = e^k - 1 - k: by its series where the difference would cancel; e = e^k - 1 from q there, and elsewhere
+    // from itself (far below zero, down to the -inf of a level that the reference bars, k + q would lose its -1)
     const float k = c.ref - r.logp;
     float q = 1.f / 3628800;
     q = q * k + 1.f / 362880;
@@ -468,12 +469,16 @@ __device__ __forceinline__ float choice_slope(const PolicyLossArgs& a, const Cho
     q = q * k + 1.f / 24;
     q = q * k + 1.f / 6;
     q = (q * k + 0.5f) * k * k;
+    float e = k + q;
     if (__builtin_amdgcn_ballot_w64(!(fabsf(k) < 1.f))) {
       asm volatile("");  // (a branch, or every wave forms both)
-      if (!(fabsf(k) < 1.f)) q = (exp_fast(k) - 1.f) - k;
+      if (!(fabsf(k) < 1.f)) {
+        e = exp_fast(k) - 1.f;
+        q = e - k;
+      }
     }
     t.kl += q;
-    if (a.kl_coef != 0.f) slope -= a.kl_coef * (k + q);  // (not 0 times infinity)
+    if (a.kl_coef != 0.f) slope -= a.kl_coef * e;  // (not 0 times infinity)
   }
   return slope * a.scale;
 }

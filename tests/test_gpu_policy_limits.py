@@ -1,0 +1,116 @@
+"""The policy calls at the limits of their arguments, against 64 bits.
+
+Tolerances.  u = 2^-24 is half a step of float32.  A row's sum of exponentials is off, relative to itself, by
+
+  the additions one after another: one fewer than a lane has values, 6 steps over the lanes of a wave, one fewer than
+    there are waves;
+  3 u for every round that a workgroup's thread takes of a row, whose running sum is brought to a new maximum;
+  the exponentials, 2 u each and (rounded difference, rounded product, the constant in it) 2.22 u for every unit of the
+    distance from the maximum, whose mean under the row's probabilities is at most log(levels):
+
+sum_bound below, in u: 38 at 1024 levels, 56 at 2048, 74 at 8192, 191 at 65536.  A log-probability d - log(sum) adds the rounding of
+d, of the logarithm (2 u of it) and of the difference: (2 |d| + 3 |log sum| + sum_bound) u.
+
+A gradient's value is made of products (slope of a choice) x (probability).  A slope holds exponentials of a
+log-probability minus another number z: that log-probability's error, 3.22 u |z| of the difference, the product and the
+constant, and 6 u of the exponential and the products; z reaches 8 upwards, and below zero e^z loses what |z| gains
+against the 1 beside it.  A probability: 2.22 u |d| + (sum_bound + 5) u.  The sum over S slopes S u, what remains 8 u.
+All of it relative to the parts' sizes as the oracle adds them up.
+"""
+
+import numpy as np
+import pytest
+
+import oracle.training as ot
+from test_gpu_policy import U, dev, host, loss_inputs, rng
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lrb():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2306_11268_amd import binding
+    binding.load()
+    return binding
+
+
+def sum_bound(k):
+    values, waves, rounds = (16, 1, 0) if k <= 1024 else (32, 1, 0) if k <= 2048 else (32, 4, 4) if k <= 8192 else (128, 8, 8)
+    return values - 1 + 6 + waves - 1 + 3 * rounds + 2 + 2.22 * np.log(k)
+
+
+def distances(x):
+    x = x.astype(np.float64)
+    d = x - x.max(-1, keepdims=True)
+    return d, np.log(np.exp(d).sum(-1))
+
+
+def check_logp(x, a, got):
+    d, lz = distances(x)
+    want = ot.policy_logp(x, a)
+    da = np.take_along_axis(d, a.T, axis=1).T
+    tol = (2 * np.abs(da) + 3 * np.abs(lz) + sum_bound(x.shape[1])) * U
+    assert np.all(np.abs(got - want) <= tol), np.max(np.abs(got - want) / tol)
+
+
+def parts_bound(x, s):
+    d, lz = distances(x)
+    far = np.abs(d[np.isfinite(d)]).max()
+    b = sum_bound(x.shape[1])
+    return (2 * far + 3 * lz.max() + b + 3.22 * 8 + 6 + 2.22 * far + b + 5 + s + 8) * U
+
+
+@pytest.mark.parametrize("k", (3, 16, 40, 100, 256, 1500, 3000, 6000, 40007))
+@pytest.mark.parametrize("far", (-np.inf, -1e30, -1e8, -1000.0, -100.0))
+def test_references_far_below_the_policy(lrb, k, far):
+    """d = ref_logp - logp from far below zero to 8: dl/dlogp has kl_coef (1 - e^d), which is kl_coef where the reference
+    bars the level, however large e^d - d - 1 is there."""
+    g = rng(20, k)
+    r, s = 9, 5
+    x, a, old, adv, _ = loss_inputs(g, r, k, s, True, True)
+    ref = (ot.policy_logp(x, a) + g.uniform(-30.0, 8.0, a.shape)).astype(np.float32)
+    hit = g.uniform(size=a.shape) < 0.4
+    hit[0, 0] = True
+    ref[hit] = far
+    a[2, 5] = a[0, 3] = -1
+    kw = dict(clip_low=0.2, clip_high=0.28, kl_coef=0.1, entropy_coef=0.05, scale=1.0 / a.size)
+    with np.errstate(invalid="ignore"):
+        want, terms, grad, size, sizes = ot.policy_loss(x, a, old, adv, ref_logp=ref, **kw)
+    parts = parts_bound(x, s)
+    t_tol = parts * sizes + U * np.abs(terms)
+    for dt, half in ((torch.float32, U), (torch.bfloat16, 2.0 ** -8)):
+        loss, got_terms, got = lrb.lr_policy_loss(dev(x), dev(a), dev(old), dev(adv), ref_logp=dev(ref), grad_dtype=dt, **kw)
+        got, got_terms = host(got), host(got_terms)
+        assert np.isfinite(got).all()
+        off, tol = np.abs(got - grad), parts * size + half * np.abs(grad) + 1e-40
+        assert np.all(off <= tol), (off / tol).max()
+        fine = [0, 2, 3] if np.isinf(far) else [0, 1, 2, 3]
+        assert np.all(np.abs(got_terms[fine] - terms[fine]) <= t_tol[fine] + 1e-40), (got_terms, terms)
+        if np.isinf(far):
+            assert got_terms[1] == np.inf and float(loss) == np.inf
+        else:
+            assert abs(float(loss) - want) <= t_tol[0] + 0.1 * t_tol[1] + 0.05 * t_tol[2] + U * abs(want)
+    # no KL term in the loss: the reference is only reported
+    loss, got_terms, got = lrb.lr_policy_loss(dev(x), dev(a), dev(old), dev(adv), ref_logp=dev(ref), **dict(kw, kl_coef=0.0))
+    assert np.isfinite(float(loss)) and np.isfinite(host(got)).all()
+
+
+def test_a_step_with_a_reference_that_bars_drawn_levels(lrb):
+    """The reference policy's own log-probabilities, -inf where it bars a level: the step is taken."""
+    g = rng(21)
+    x = dev(g.standard_normal((50, 12)).astype(np.float32))
+    before = x.clone()
+    ref_scores = x.clone()
+    ref_scores[:, 4] = -np.inf
+    t = lrb.TrainTensors([x], [torch.zeros_like(x)])
+    a, lp, _ = lrb.lr_policy_draw(x, dev(g.gumbel(size=(8, 50, 12)).astype(np.float32)))
+    ref = lrb.lr_policy_logp(ref_scores, a)
+    assert bool(torch.isinf(ref).any())
+    _, _, norm = lrb.policy_train_step(t, a, lp, dev(g.standard_normal(8).astype(np.float32)), 1, lr=0.1, ref_logp=ref,
+                                       kl_coef=0.1)
+    assert np.isfinite(float(norm)) and not torch.equal(x, before)
+    assert bool(torch.isfinite(x).all())
