@@ -697,7 +697,7 @@ __global__ void __launch_bounds__(kPolicyThreads, WAVES) policy_loss_rows_kernel
         asm volatile("");
         if (c.act >= K) {
           ratio.spoil();
-          add.entropy = add.cut = __builtin_nanf("");
+          add.kl = add.entropy = add.cut = __builtin_nanf("");
         }
       }
       // undecided choices: the wave forms their rows' sums again, in 64 bits
@@ -877,7 +877,7 @@ __global__ void __launch_bounds__(THREADS, 4) policy_loss_long_kernel(PolicyLoss
       Ratio ratio(a, c, floor_d(x - m), lz);
       if (c.act >= K) {
         ratio.spoil();
-        add.entropy = add.cut = __builtin_nanf("");
+        add.kl = add.entropy = add.cut = __builtin_nanf("");
       }
       const bool here = real && ratio.open(c, open_row(lz));
       near |= here;

@@ -114,3 +114,17 @@ def test_a_step_with_a_reference_that_bars_drawn_levels(lrb):
                                        kl_coef=0.1)
     assert np.isfinite(float(norm)) and not torch.equal(x, before)
     assert bool(torch.isfinite(x).all())
+
+
+@pytest.mark.parametrize("k", (2, 16, 60, 300, 2000, 5000, 40007))
+@pytest.mark.parametrize("reference", (False, True))
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_an_action_out_of_range_shows_in_every_term(lrb, k, reference, dtype):
+    x, a, old, adv, ref = loss_inputs(rng(22, k), 9, k, 3, False, reference)
+    a[1, 4] = k
+    for kl in (0.0, 0.1):
+        loss, terms, grad = lrb.lr_policy_loss(dev(x), dev(a), dev(old), dev(adv), kl_coef=kl, entropy_coef=0.1,
+                                               ref_logp=dev(ref) if reference else None, grad_dtype=dtype)
+        assert np.isnan(float(loss)) and np.all(np.isnan(host(terms)))
+        bad = np.isnan(host(grad))
+        assert bad[4].all() and not np.delete(bad, 4, axis=0).any()
