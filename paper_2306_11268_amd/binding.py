@@ -626,11 +626,8 @@ def lr_policy_loss(logits, actions, old_logp, advantages, ref_logp=None, clip_lo
         raise ValueError(f"grad_dtype must be float32 or bfloat16, got {grad_dtype}")
     if want_grad and out_grad is None:
         out_grad = torch.empty(logits.shape, dtype=grad_dtype, device=dev)
-    new = torch.empty
-    if s * count == 0:  # the call enqueues nothing: the loss and the gradient of no choices
-        new = torch.zeros
-        if out_grad is not None:
-            out_grad.zero_()
+    nothing = s * count == 0  # no choices: the call enqueues nothing, the loss and the gradient are zero
+    new = torch.zeros if nothing else torch.empty
     loss = new((), dtype=torch.float32, device=dev) if want_loss else None
     terms = new(4, dtype=torch.float32, device=dev) if want_loss else None
     work = torch.empty(int(load().lr_policy_workspace_size()), dtype=torch.uint8, device=dev)
@@ -646,6 +643,8 @@ def lr_policy_loss(logits, actions, old_logp, advantages, ref_logp=None, clip_lo
                    LR_GRAD_BF16 if grad_dtype == torch.bfloat16 else LR_GRAD_F32,
                    _at(dev, out_grad, grad_dtype, logits.shape, "grad_logits"), work.data_ptr(), work.numel()),
            "lr_policy_loss")
+    if nothing and out_grad is not None:
+        out_grad.zero_()
     return loss, terms, out_grad
 
 

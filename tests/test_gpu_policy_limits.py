@@ -128,3 +128,22 @@ def test_an_action_out_of_range_shows_in_every_term(lrb, k, reference, dtype):
         assert np.isnan(float(loss)) and np.all(np.isnan(host(terms)))
         bad = np.isnan(host(grad))
         assert bad[4].all() and not np.delete(bad, 4, axis=0).any()
+
+
+@pytest.mark.parametrize("rollouts,pixels", [(0, 5), (3, 0), (3, 5)])
+def test_a_refused_loss_leaves_its_outputs(lrb, rollouts, pixels):
+    x = torch.ones((pixels, 16), device="cuda")
+    a = torch.zeros((rollouts, pixels), dtype=torch.int32, device="cuda")
+    old, adv = torch.zeros((rollouts, pixels), device="cuda"), torch.ones(rollouts, device="cuda")
+    out = torch.full((7, 16), 3.0, device="cuda")
+    fit = out[:pixels]
+    for args, kw in (((x, a, old.double(), adv), dict(out_grad=fit)), ((x, a.long(), old, adv), dict(out_grad=fit)),
+                     ((x, a, old, adv[:0] if rollouts else torch.ones(2, device="cuda")), dict(out_grad=fit)),
+                     ((x, a, old, adv), dict(out_grad=fit, ref_logp=old.half())),
+                     ((x, a, old, adv), dict(out_grad=out)),
+                     ((x, a, old, adv), dict(out_grad=fit, grad_dtype=torch.bfloat16))):
+        with pytest.raises(ValueError):
+            lrb.lr_policy_loss(*args, **kw)
+    with pytest.raises(lrb.LrError):
+        lrb.lr_policy_loss(x, a, old, adv, out_grad=fit, clip_low=2.0)
+    assert bool((out == 3.0).all())
