@@ -628,7 +628,8 @@ def lr_policy_loss(logits, actions, old_logp, advantages, ref_logp=None, clip_lo
         out_grad = torch.empty(logits.shape, dtype=grad_dtype, device=dev)
     nothing = s * count == 0  # no choices: the call enqueues nothing, the loss and the gradient are zero
     new = torch.zeros if nothing else torch.empty
-    loss = new((), dtype=torch.float32, device=dev) if want_loss else None
+    # (a gradient without values has no address, and the call wants an output)
+    loss = new((), dtype=torch.float32, device=dev) if want_loss or (nothing and out_grad is not None) else None
     terms = new(4, dtype=torch.float32, device=dev) if want_loss else None
     work = torch.empty(int(load().lr_policy_workspace_size()), dtype=torch.uint8, device=dev)
     policy = LrPolicy(clip_low, clip_high, kl_coef, entropy_coef, 1.0 / max(1, s * count) if scale is None else scale)
@@ -638,14 +639,14 @@ def lr_policy_loss(logits, actions, old_logp, advantages, ref_logp=None, clip_lo
                    _at(dev, old_logp, torch.float32, shape, "old_logp"),
                    _at(dev, ref_logp, torch.float32, shape, "ref_logp"),
                    _at(dev, advantages, torch.float32, shape if per_choice else (s,), "advantages"),
-                   1 if per_choice else 0, s, count, k, loss.data_ptr() if want_loss else None,
-                   terms.data_ptr() if want_loss else None,
+                   1 if per_choice else 0, s, count, k, None if loss is None else loss.data_ptr(),
+                   None if terms is None else terms.data_ptr(),
                    LR_GRAD_BF16 if grad_dtype == torch.bfloat16 else LR_GRAD_F32,
                    _at(dev, out_grad, grad_dtype, logits.shape, "grad_logits"), work.data_ptr(), work.numel()),
            "lr_policy_loss")
     if nothing and out_grad is not None:
         out_grad.zero_()
-    return loss, terms, out_grad
+    return loss if want_loss else None, terms, out_grad
 
 
 class TrainTensors:

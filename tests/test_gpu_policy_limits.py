@@ -147,3 +147,14 @@ def test_a_refused_loss_leaves_its_outputs(lrb, rollouts, pixels):
     with pytest.raises(lrb.LrError):
         lrb.lr_policy_loss(x, a, old, adv, out_grad=fit, clip_low=2.0)
     assert bool((out == 3.0).all())
+
+
+@pytest.mark.parametrize("rollouts,pixels", [(0, 5), (3, 0), (0, 0)])
+def test_a_gradient_of_no_choices_alone(lrb, rollouts, pixels):
+    x = torch.ones((pixels, 16), device="cuda")
+    a = torch.zeros((rollouts, pixels), dtype=torch.int32, device="cuda")
+    old, adv = torch.zeros((rollouts, pixels), device="cuda"), torch.ones(rollouts, device="cuda")
+    loss, terms, grad = lrb.lr_policy_loss(x, a, old, adv, want_loss=False)
+    assert loss is None and terms is None and grad.shape == x.shape and not bool(grad.any())
+    loss, terms, grad = lrb.lr_policy_loss(x, a, old, adv, want_grad=False)
+    assert float(loss) == 0 and not bool(terms.any()) and grad is None
