@@ -158,3 +158,46 @@ def test_a_gradient_of_no_choices_alone(lrb, rollouts, pixels):
     assert loss is None and terms is None and grad.shape == x.shape and not bool(grad.any())
     loss, terms, grad = lrb.lr_policy_loss(x, a, old, adv, want_grad=False)
     assert float(loss) == 0 and not bool(terms.any()) and grad is None
+
+
+@pytest.mark.parametrize("k,rows", [(2051, 9), (5000, 6), (8192, 5), (10007, 4), (40007, 3)])
+@pytest.mark.parametrize("s", (4, 5, 7, 8, 9, 13))
+def test_draws_of_many_rollouts_from_long_rows(lrb, k, rows, s):
+    """More rollouts than one pass over the scores takes, and groups of them that are not full."""
+    g = rng(23, k, s)
+    x = (2 * g.standard_normal((rows, k))).astype(np.float32)
+    noise = g.gumbel(size=(s, rows, k)).astype(np.float32)
+    noise[-1, 0, k - 1] = 100.0  # the last level, of the last rollout
+    noise[s // 2, 1] = -np.inf   # (every score equal: the first)
+    levels = g.uniform(0, 6, k).astype(np.float32)
+    a, lp, phi = lrb.lr_policy_draw(dev(x), dev(noise), dev(levels))
+    want = ot.policy_draw(x, noise)
+    assert want[-1, 0] == k - 1 and want[s // 2, 1] == 0
+    assert np.array_equal(host(a), want) and np.array_equal(host(phi), levels[want])
+    check_logp(x, want, host(lp))
+    # each rollout drawn alone gives the same
+    for i in range(s):
+        one = lrb.lr_policy_draw(dev(x), dev(noise[i:i + 1]))
+        assert torch.equal(one[0][0], a[i]) and torch.equal(one[1][0], lp[i])
+
+
+def test_draws_of_more_long_rows_than_workgroups(lrb):
+    k, rows, s, n = 2051, 65536 + 97, 5, 61
+    g = rng(24)
+    x = dev((2 * g.standard_normal((n, k))).astype(np.float32))
+    noise = dev(g.gumbel(size=(s, n, k)).astype(np.float32))
+    small = lrb.lr_policy_draw(x, noise)
+    assert np.array_equal(host(small[0]), ot.policy_draw(host(x), host(noise)))
+    first = torch.arange(rows, device="cuda") % n
+    big = lrb.lr_policy_draw(x[first], noise[:, first])
+    assert torch.equal(big[0], small[0][:, first]) and torch.equal(big[1], small[1][:, first])
+
+
+@pytest.mark.parametrize("k", (100, 2000, 3000, 10007))
+@pytest.mark.parametrize("s", (257, 513, 1024))
+def test_log_probabilities_of_more_rollouts_than_threads(lrb, k, s):
+    g = rng(25, k, s)
+    x = (2 * g.standard_normal((3, k))).astype(np.float32)
+    a = g.integers(0, k, (s, 3)).astype(np.int32)
+    a[0], a[-1] = 0, k - 1
+    check_logp(x, a, host(lrb.lr_policy_logp(dev(x), dev(a))))
