@@ -715,11 +715,14 @@ class TrainTensors:
         self.grad_type = LR_GRAD_BF16 if dtype == torch.bfloat16 else LR_GRAD_F32
 
     def first(self):
-        """The first parameter and its gradient, which must be where they were when they were given."""
-        p, g = self.params[0], self.grads[0]
-        if (p.data_ptr(), g.data_ptr()) != (self._table[0], self._table[1]):
-            raise ValueError("a tensor has other memory than when it was given")
-        return p, g
+        """The first parameter and its gradient.  Every tensor must be where it was when it was given."""
+        kinds = {"d_param": self.params, "d_grad": self.grads, "d_m": self.m, "d_v": self.v}
+        if self.bits == 8:
+            kinds["d_scales"] = self.scales
+        for field, tensors in kinds.items():
+            if [t.data_ptr() for t in tensors] != self._table[self._FIELDS.index(field)::len(self._FIELDS)]:
+                raise ValueError(f"{field}: a tensor has other memory than when it was given")
+        return self.params[0], self.grads[0]
 
 
 def lr_grad_norm(grads, out=None):
