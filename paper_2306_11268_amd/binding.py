@@ -537,7 +537,7 @@ def multichannel_train_step(nets, amps, phis, saveds, labels, kind: int = LR_LOS
 def _run_on(device, fn, *args) -> int:
     """fn(*args, stream) with the device current and on its current stream."""
     torch = _torch()
-    if torch.cuda.current_device() != device.index:
+    if torch._C._cuda_getDevice() != device.index:  # (a tensor is there: the runtime has started)
         with torch.cuda.device(device):
             return fn(*args, _stream(device))
     # (the stream's handle without the Python object around it, which takes 2 us)
@@ -656,7 +656,8 @@ class TrainTensors:
     all float32 or all bfloat16.  bits: 32 or 8, of the moments, which are
     allocated as zeros unless m, v (and for 8 bits scales) are given.  The
     object keeps the tensors' memory: their values may change between steps,
-    and set_grads puts other gradients in place."""
+    and set_grads puts other gradients in place.  A tensor whose .data is
+    replaced is not followed, and one whose storage is resized is refused."""
 
     _FIELDS = ("d_param", "d_grad", "d_m", "d_v", "d_scales", "count")
 
@@ -669,6 +670,8 @@ class TrainTensors:
         # lr_param [num], field by field
         self._table = (c_int64 * (len(self._FIELDS) * max(self.num, 1)))()
         self._held = {}
+        self._at_of = torch.UntypedStorage.data_ptr
+        self._memory = {}  # of each kind: the storages' addresses and the storages, each once
         like = grads if params is None else params
         self.device = like[0].device if self.num else torch.device("cuda", torch.cuda.current_device())
         self._counts = [t.numel() for t in like]
@@ -702,7 +705,10 @@ class TrainTensors:
                 raise ValueError(f"{field}: a contiguous {dtype} tensor of {n} values on {dev} is needed, "
                                  f"got {t.dtype} {tuple(t.shape)} on {t.device}")
         # (the memory stays with this object, whatever becomes of the caller's tensors)
-        self._held[field] = [t.untyped_storage() for t in tensors]
+        held = self._held[field] = [t.untyped_storage() for t in tensors]
+        once = dict(zip(map(self._at_of, held), held))
+        once.pop(0, None)  # (of tensors without values)
+        self._memory[field] = list(once), list(once.values())
         self._set(field, [t.data_ptr() for t in tensors])
         return tensors
 
@@ -713,6 +719,15 @@ class TrainTensors:
             raise ValueError(f"gradients must be float32 or bfloat16, got {dtype}")
         self.grads = self._hold("d_grad", grads, dtype, self._counts)
         self.grad_type = LR_GRAD_BF16 if dtype == torch.bfloat16 else LR_GRAD_F32
+
+    def table(self, *fields):
+        """The lr_param table for a call that uses these fields (all: none given).  The memory of a storage that was
+        resized is not the one that the table points to any more: refused."""
+        at_of = self._at_of
+        for field, (at, storages) in self._memory.items():
+            if (not fields or field in fields) and [*map(at_of, storages)] != at:
+                raise ValueError(f"{field}: a storage was resized, and the memory of its tensors is gone")
+        return self._table
 
     def first(self):
         """The first parameter and its gradient.  Every tensor must be where it was when it was given."""
@@ -733,7 +748,7 @@ def lr_grad_norm(grads, out=None):
     if out is None:
         out = torch.empty((), dtype=torch.float32, device=t.device)
     work = torch.empty(int(load().lr_grad_norm_workspace_size(t.num)), dtype=torch.uint8, device=t.device)
-    _check(_run_on(t.device, load().lr_grad_norm, t._table, t.num, t.grad_type,
+    _check(_run_on(t.device, load().lr_grad_norm, t.table("d_grad"), t.num, t.grad_type,
                    _at(t.device, out, torch.float32, (), "norm"), work.data_ptr(), work.numel()), "lr_grad_norm")
     return out
 
@@ -750,7 +765,7 @@ def lr_adamw_update(tensors: TrainTensors, step: int, lr: float, beta1: float = 
         raise ValueError("these tensors have no parameters")
     if step >= 1 << 31:
         raise ValueError(f"step {step} is beyond 32 bits")
-    _check(_run_on(tensors.device, load().lr_adamw_update, tensors._table, tensors.num, tensors.grad_type,
+    _check(_run_on(tensors.device, load().lr_adamw_update, tensors.table(), tensors.num, tensors.grad_type,
                    LR_STATE_8BIT if tensors.bits == 8 else LR_STATE_F32, int(step), lr, beta1, beta2, eps,
                    weight_decay, _at(tensors.device, norm, torch.float32, (), "norm"), max_norm,
                    (int(step) if seed is None else int(seed)) & 0xFFFFFFFF), "lr_adamw_update")
@@ -775,8 +790,8 @@ def lr_adamw_moments(tensors: TrainTensors, out_m=None, out_v=None):
         outs.append(list(given))
     at = [(c_void_p * max(tensors.num, 1))(*[_at(tensors.device, t, torch.float32, (n,), "moments")
                                              for t, n in zip(o, tensors._counts)]) for o in outs]
-    _check(_run_on(tensors.device, load().lr_adamw_moments, tensors._table, tensors.num, at[0], at[1]),
-           "lr_adamw_moments")
+    _check(_run_on(tensors.device, load().lr_adamw_moments, tensors.table("d_m", "d_v", "d_scales"), tensors.num,
+                   at[0], at[1]), "lr_adamw_moments")
     return outs[0], outs[1]
 
 

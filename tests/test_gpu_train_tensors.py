@@ -45,3 +45,56 @@ def test_a_policy_step_refuses_any_tensor_that_moved(lrb, which, i):
     t.set_grads(grads)
     lrb.policy_train_step(t, a, lp, adv, 1, lr=0.1)
     assert bool(params[1].any())
+
+
+def calls(lrb, t, field):
+    """The calls that use a field."""
+    yield lambda: lrb.lr_adamw_update(t, 1, lr=0.1)
+    if field == "grads":
+        yield lambda: lrb.lr_grad_norm(t)
+    if field in ("m", "v", "scales") and t.bits == 8:
+        yield lambda: lrb.lr_adamw_moments(t)
+
+
+@pytest.mark.parametrize("bits,field", [(bits, f) for bits in (32, 8) for f in ("params", "grads", "m", "v", "scales")
+                                        if bits == 8 or f != "scales"])
+@pytest.mark.parametrize("size", (0, 16, 1 << 16))
+def test_a_resized_storage_is_refused(lrb, bits, field, size):
+    """Its memory has gone back to the allocator: the addresses that the object holds are no longer its own."""
+    ones = lambda: [torch.ones(700, device="cuda") for _ in range(3)]  # noqa: E731
+    p, g = ones(), ones()
+    t = lrb.TrainTensors(p, g, bits=bits)
+    for call in calls(lrb, t, field):
+        call()
+    tensors = getattr(t, field)
+    others = [z for z in (*p, *g, *t.m, *t.v) if z is not tensors[1]]
+    before = [z.clone() for z in others]
+    tensors[1].untyped_storage().resize_(size)
+    for call in calls(lrb, t, field):
+        with pytest.raises(ValueError):
+            call()
+    assert all(torch.equal(a, b) for a, b in zip(others, before))
+
+
+def test_gradients_put_in_place_of_resized_ones(lrb):
+    g = [torch.ones(700, device="cuda") for _ in range(3)]
+    t = lrb.TrainTensors(None, g)
+    g[2].untyped_storage().resize_(0)
+    with pytest.raises(ValueError):
+        lrb.lr_grad_norm(t)
+    t.set_grads([torch.ones(700, device="cuda") for _ in range(3)])
+    assert abs(float(lrb.lr_grad_norm(t)) - 2100 ** 0.5) < 1e-5
+
+
+def test_tensors_that_share_a_storage_or_have_no_values(lrb):
+    flat = torch.ones(1000, device="cuda")
+    p = [flat[:300], torch.zeros(0, device="cuda"), flat[300:]]
+    g = [torch.ones(300, device="cuda"), torch.zeros(0, device="cuda"), torch.ones(700, device="cuda")]
+    t = lrb.TrainTensors(p, g)
+    lrb.lr_adamw_update(t, 1, lr=0.1)
+    p[1].untyped_storage().resize_(64)  # (an empty tensor has nothing to lose)
+    lrb.lr_adamw_update(t, 2, lr=0.1)
+    assert bool((flat < 1).all())
+    flat.untyped_storage().resize_(0)
+    with pytest.raises(ValueError):
+        lrb.lr_adamw_update(t, 3, lr=0.1)
