@@ -763,7 +763,7 @@ def lr_adamw_update(tensors: TrainTensors, step: int, lr: float, beta1: float = 
     torch = _torch()
     if tensors.params is None:
         raise ValueError("these tensors have no parameters")
-    if step >= 1 << 31:
+    if not -(1 << 31) <= step < 1 << 31:
         raise ValueError(f"step {step} is beyond 32 bits")
     _check(_run_on(tensors.device, load().lr_adamw_update, tensors.table(), tensors.num, tensors.grad_type,
                    LR_STATE_8BIT if tensors.bits == 8 else LR_STATE_F32, int(step), lr, beta1, beta2, eps,

@@ -98,3 +98,15 @@ def test_tensors_that_share_a_storage_or_have_no_values(lrb):
     flat.untyped_storage().resize_(0)
     with pytest.raises(ValueError):
         lrb.lr_adamw_update(t, 3, lr=0.1)
+
+
+def test_steps_beyond_32_bits_either_way_are_refused(lrb):
+    p = torch.ones(8, device="cuda")
+    t = lrb.TrainTensors([p], [torch.ones(8, device="cuda")])
+    for step in (-(1 << 32) + 5, -(1 << 31) - 1, 1 << 31, (1 << 32) + 5):
+        with pytest.raises(ValueError):
+            lrb.lr_adamw_update(t, step, lr=0.1)
+    for step in (0, -1, -(1 << 31)):
+        with pytest.raises(lrb.LrError):
+            lrb.lr_adamw_update(t, step, lr=0.1)
+    assert bool((p == 1).all())
