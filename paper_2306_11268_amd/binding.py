@@ -665,6 +665,8 @@ class TrainTensors:
         torch = _torch()
         if bits not in (8, 32):
             raise ValueError("bits must be 8 or 32")
+        if params is not None and len(params) != len(grads):
+            raise ValueError(f"{len(params)} parameters for {len(grads)} gradients")
         self.bits = bits
         self.num = len(grads)
         # lr_param [num], field by field
