@@ -462,8 +462,8 @@ int lr_grad_norm(const lr_param* params, int32_t num, int32_t grad_type, float* 
  *       - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
  * with norm = d_norm[0] as lr_grad_norm leaves it, read when the step runs; a
  * norm that is not finite leaves every tensor as it was, and a NULL d_norm
- * clips nothing.  step counts from 1; a captured call repeats its step and
- * seed.  state_type:
+ * clips nothing.  An eps below 2^-126 other than 0 counts as 2^-126.  step
+ * counts from 1; a captured call repeats its step and seed.  state_type:
  *   LR_STATE_F32   d_m, d_v float32, zero before step 1
  *   LR_STATE_8BIT  d_m, d_v one byte a value and d_scales, all zero before
  *     step 1.  The LR_STATE_BLOCK values from a multiple of LR_STATE_BLOCK on

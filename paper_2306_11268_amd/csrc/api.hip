@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <complex>
 #include <cstdio>
@@ -1488,7 +1489,8 @@ int lr_adamw_update(const lr_param* params, int32_t num, int32_t grad_type, int3
     a.keep = static_cast<float>(1.0 - static_cast<double>(lr) * static_cast<double>(weight_decay));
     a.rate = static_cast<float>(static_cast<double>(lr) / bc1);
     a.root = static_cast<float>(1.0 / std::sqrt(bc2));
-    a.eps = eps;
+    // (1 / eps stays finite, so that a value without moments stays where it is; beside a root above zero it is nothing)
+    a.eps = eps > 0.f ? std::max(eps, FLT_MIN) : eps;
     a.bf16 = grad_type == LR_GRAD_BF16 ? 1 : 0;
     a.bits8 = bits8 ? 1 : 0;
     hipStream_t st = static_cast<hipStream_t>(stream);

@@ -110,3 +110,17 @@ def test_steps_beyond_32_bits_either_way_are_refused(lrb):
         with pytest.raises(lrb.LrError):
             lrb.lr_adamw_update(t, step, lr=0.1)
     assert bool((p == 1).all())
+
+
+@pytest.mark.parametrize("bits", (32, 8))
+@pytest.mark.parametrize("eps", (1e-45, 1e-40, 2.0 ** -127, 2.0 ** -126))
+def test_a_subnormal_eps_does_not_move_values_without_gradient(lrb, bits, eps):
+    """0 / (0 + eps) is 0; beside a second moment above zero (its root is past 1e-23) such an eps is nothing."""
+    g = torch.linspace(-1, 1, 601, device="cuda")
+    g[::3] = 0
+    p, q = torch.ones(601, device="cuda"), torch.ones(601, device="cuda")
+    lrb.lr_adamw_update(lrb.TrainTensors([p], [g], bits=bits), 1, lr=0.1, eps=eps, weight_decay=0.5)
+    lrb.lr_adamw_update(lrb.TrainTensors([q], [g], bits=bits), 1, lr=0.1, eps=0.0, weight_decay=0.5)
+    still = g == 0
+    assert bool((p[still] == np.float32(1 - float(np.float32(0.1)) * 0.5)).all())
+    assert torch.equal(p[~still], q[~still])
