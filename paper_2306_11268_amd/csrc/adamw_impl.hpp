@@ -146,7 +146,9 @@ __global__ void __launch_bounds__(1024) grad_norm_finish_kernel(const double* __
   s = block_sum_d<1024>(s, red);
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
-// A few chunks: one workgroup, one launch.
+// A few chunks: one workgroup, one launch (one tensor of 4096, 16384, 32768, 49152
+// values: 2.5, 3.2, 4.2, 5.3 us so, 4.0, 4.3, 4.5, 4.5 with partial sums and a second
+// launch; three tensors of together six chunks 4.4, 4.5, of twelve 6.0, 4.7).
 constexpr int kNormOneValues = 32768;
 constexpr int kNormOneThreads = kNormChunk / 4;
 __global__ void __launch_bounds__(kNormOneThreads) grad_norm_one_kernel(GradList l, int bf16, float* norm) {
@@ -199,7 +201,10 @@ __device__ __forceinline__ uint32_t wave_max_bits(uint32_t x) {
   return max((uint32_t)r[0], (uint32_t)r[1]);
 }
 
-// m and v after the step, p moved by them.
+// m and v after the step, p moved by them.  The root and the reciprocal are the
+// hardware's instructions, each within one step of float32 (the exact ones take
+// some ten instructions more each): with the other roundings the change is within
+// 10 half steps of the formula's, and nothing that is kept builds on it but p.
 __device__ __forceinline__ void adamw_values(const AdamwArgs& a, float clip, const float (&g4)[4], float (&m)[4],
                                              float (&v)[4], float (&p)[4]) {
   float root[4];

@@ -6,8 +6,8 @@
 // many lanes as keep N at 4 to 16 (32 past 1024 levels): several rows share a
 // wave, so that the steps of a reduction over lanes serve all of them at once.
 // A longer row takes a workgroup.  Memory bounds them (a large copy reaches 5.0
-// TB/s on this card): draws of four rollouts for 200000 x 256 logits 180 us (5.7
-// TB/s, reading only), log-probabilities of eight for 612500 x 64 43 us, the
+// TB/s on this card): draws of four rollouts for 200000 x 256 logits 175 us (5.9
+// TB/s, reading only), log-probabilities of eight for 612500 x 64 41 us, the
 // loss and gradient of 16 rollouts for 200000 x 256 97 us (4.6 TB/s).
 #pragma once
 
@@ -439,10 +439,15 @@ struct Ratio {
     over = ratio - border;
     over = up ? over : -over;
   }
-  // So near to the border that float32 may put it on the wrong side: the errors
-  // of the log-probability (of d, the sum of exponentials and its logarithm)
-  // reach over it.  There the log-probability is within 90 of old, and |d|
-  // within lz of the log-probability.  row: of open_row.
+  // So near to the border that float32 may put it on the wrong side.  With u = 2^-24 the ratio is off, relative to
+  // itself, by
+  //   |d| u + |logp| u       the roundings of d and of logp = d - lz (|d| <= |logp| + lz),
+  //   2 lz u + s u           the logarithm, and the sum of exponentials before it: 191 u at 65536 levels (128 values of
+  //                          a lane one after another, 6 steps of lanes, 7 of waves, 3 u in each of 8 rounds for a new
+  //                          maximum, and 2 u + 2.22 u |d| of an exponential, |d| log 65536 in the mean at most),
+  //   3.3 |logp - old| u + 4 u  the difference, its exponential and the border.
+  // logp is at most 0 and the border at least u or 0, so logp - old is at least -16.7 beside a border, and at most |old|:
+  // together within (3.3 |old| + 3 lz + 290) u.  row (of open_row) and the factor of |old| hold 436 u + 6 u lz and 6 u.
   __device__ __forceinline__ bool open(const Choice& c, float row) const {
     return fabsf(over) <= border * fmaf(fabsf(c.old), 3.6e-7f, row);
   }
@@ -1001,11 +1006,14 @@ static void policy_rows_shape(int K, F&& rows) {
   else rows(Shape<64, 32, TAIL>{});
 }
 // The loss's rows: also how many threads of a row add slopes, and the
-// workgroups that a CU holds by their registers (without spilling any but two up
-// to 32 levels, where a sixth workgroup gives 3 %).  With tables every thread of
-// a workgroup takes choices up to 24 levels, and half of them above, so rows share
-// few lanes: 32 rollouts of 612500 x 24 105 us with four lanes a row, 88 with two;
-// 16 of 400000 x 40 66 with eight, 51 with four, of 400000 x 64 82, 80.
+// workgroups that a CU holds by their registers (without spilling any but two or
+// three at 25 to 32 levels, where a sixth workgroup gives 3 %).  With tables every
+// thread of a workgroup takes choices up to 24 levels, and half of them above, so
+// rows share few lanes: 16 rollouts of 612500 x 17, 20, 24 61, 58, 59 us with four
+// lanes a row, 49, 48, 50 with two, 32 rollouts of 612500 x 20 100, 85; 16 of 400000
+// x 40 66 with eight, 51 with four, of 400000 x 64 82, 80.  Up to 48 levels rows of 12
+// values a lane, not 16: 16 rollouts of 400000 x 33, 36, 40, 47, 48 55, 51, 52, 58, 52
+// us with 16, 50, 47, 50, 55, 51 with 12.
 template <int G_, int N_, int PARTS_, int WAVES_, bool TAIL_>
 struct LossShape {
   static constexpr int G = G_, N = N_, PARTS = PARTS_, WAVES = WAVES_;
@@ -1085,8 +1093,8 @@ hipError_t launch_policy_loss(const PolicyLossArgs& a, hipStream_t st) {
   };
   if (a.K > kPolicyRowMax) {
     grid = dim3((unsigned)std::min<long long>(a.count, kPolicyParts));
-    // (Rounds held: what 128 registers a lane take, the most of which are a row's values; with a fourth round, or
-    // with 80 registers for six waves on a SIMD, the compiler spills.  1600 rows of 40007 in bf16 111 us with four
+    // (Rounds held: what 128 registers a lane take, the most of which are a row's values, but for two or three that
+    // workgroups of 128 and 256 spill; with a fourth round, or with 80 registers for six waves on a SIMD, many more.  1600 rows of 40007 in bf16 111 us with four
     // rounds, 97 with three; 1500 of 65536 194, 186.  Short rows in smaller workgroups, which wait for fewer waves:
     // 16 rollouts of 20000 x 2500 148 -> 121 us with 128 threads and two rounds after 256 with one, of 10000 x 5000
     // 134 -> 108 with 256 after 512.  1024 threads, which hold rows of 40007 whole but fill a CU alone: 139 -> 149.)
