@@ -9,6 +9,7 @@ raises if liblr.so has not been built.  There is no fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 from typing import Optional, Sequence
@@ -152,6 +153,7 @@ def _check(status: int, what: str) -> None:
 # torch marshalling helpers
 # ---------------------------------------------------------------------------
 
+@functools.lru_cache(maxsize=None)  # (the import statement alone takes 0.1 us, several times a call)
 def _torch():
     import torch
     return torch
@@ -726,9 +728,9 @@ class TrainTensors:
         """The lr_param table for a call that uses these fields (all: none given).  The memory of a storage that was
         resized is not the one that the table points to any more: refused."""
         at_of = self._at_of
-        for field, (at, storages) in self._memory.items():
-            if (not fields or field in fields) and [*map(at_of, storages)] != at:
-                raise ValueError(f"{field}: a storage was resized, and the memory of its tensors is gone")
+        for at, storages in [self._memory[f] for f in fields] if fields else self._memory.values():
+            if [*map(at_of, storages)] != at:
+                raise ValueError("a storage of these tensors was resized, and its memory is gone")
         return self._table
 
     def first(self):
