@@ -400,8 +400,9 @@ int lr_policy_logp(const float* d_logits, const int32_t* d_actions, int32_t samp
  *   dL/dlogits[r][j] = sum over the row's choices of
  *       scale ((j = action) - p_j) dl/dlogp + scale entropy_coef p_j (log p_j + H)
  * where dl/dlogp = -ratio A (0 where the clipped term is the smaller) +
- * kl_coef (1 - exp(d)).  Which side of a clip border a ratio lies on is
- * decided to about 1e-9.
+ * kl_coef (1 - exp(d)), which is kl_coef where d_ref_logp is -inf, at a level
+ * that the reference bars (the loss is infinite there).  Which side of a clip
+ * border a ratio lies on is decided to about 1e-9.
  *   d_old_logp    float32 [samples][count], when the levels were drawn
  *   d_ref_logp    nullable (no KL term), float32 [samples][count]
  *   d_advantages  float32 [samples], or with per_choice != 0 [samples][count]
@@ -463,7 +464,8 @@ int lr_grad_norm(const lr_param* params, int32_t num, int32_t grad_type, float* 
  * with norm = d_norm[0] as lr_grad_norm leaves it, read when the step runs; a
  * norm that is not finite leaves every tensor as it was, and a NULL d_norm
  * clips nothing.  An eps below 2^-126 other than 0 counts as 2^-126.  step
- * counts from 1; a captured call repeats its step and seed.  state_type:
+ * counts from 1; a captured call repeats its step and seed, replay after
+ * replay (a training step is called anew).  state_type:
  *   LR_STATE_F32   d_m, d_v float32, zero before step 1
  *   LR_STATE_8BIT  d_m, d_v one byte a value and d_scales, all zero before
  *     step 1.  The LR_STATE_BLOCK values from a multiple of LR_STATE_BLOCK on

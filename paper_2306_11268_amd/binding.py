@@ -617,7 +617,8 @@ def lr_policy_loss(logits, actions, old_logp, advantages, ref_logp=None, clip_lo
     action: no choice there); advantages [S], or [S, ...] for every choice.
     scale defaults to 1 / (S * pixels): give 1 / (choices made) for the mean
     where some are missing.  terms: scale times the sums of the clipped term,
-    of the KL estimate and of the entropy, and the clipped share."""
+    of the KL estimate (infinite where ref_logp is -inf; the gradient is not)
+    and of the entropy, and the clipped share."""
     torch = _torch()
     dev = logits.device
     s = int(actions.shape[0])
@@ -763,7 +764,8 @@ def lr_adamw_update(tensors: TrainTensors, step: int, lr: float, beta1: float = 
     """One AdamW step over all tensors, in place.  norm: lr_grad_norm's scalar;
     the gradients are then scaled down to max_norm, and a norm that is not
     finite leaves everything as it was.  seed (of the rounding of 8-bit
-    moments, a 32-bit number) defaults to the step."""
+    moments, a 32-bit number) defaults to the step.  Both are part of a
+    recorded call: a replay repeats them, so call it anew for each step."""
     torch = _torch()
     if tensors.params is None:
         raise ValueError("these tensors have no parameters")
@@ -807,7 +809,8 @@ def policy_train_step(tensors: TrainTensors, actions, old_logp, advantages, step
     The scores [..., K] are the first parameter of tensors.  The policy loss
     (policy: the arguments of lr_policy_loss) writes their gradient into
     tensors' first gradient, the norm is taken over all gradients, and the
-    clipped AdamW step moves every parameter.  Returns (loss, terms, norm)."""
+    clipped AdamW step moves every parameter.  All tensors must still be where
+    they were when tensors was made.  Returns (loss, terms, norm)."""
     if not tensors.params:
         raise ValueError("these tensors have no parameters")
     logits, grad = tensors.first()

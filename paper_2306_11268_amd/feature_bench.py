@@ -22,7 +22,8 @@ seeded synthetic workloads; the optics are those of the workloads named.
       over 5x350x350 pixels of a 16-level device, the gradient norm and the
       AdamW step with 8-bit moments over 5x350x350x256 scores with bf16
       gradients, the AdamW step over the masks of three channels, and a whole
-      step: draw, the rollouts in the emulator (batch 64), loss, norm, AdamW.
+      step: draw (from noise that is there already), the rollouts in the
+      emulator (batch 64), loss, norm, AdamW.
 """
 
 from __future__ import annotations
