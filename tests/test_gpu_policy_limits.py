@@ -201,3 +201,28 @@ def test_log_probabilities_of_more_rollouts_than_threads(lrb, k, s):
     a = g.integers(0, k, (s, 3)).astype(np.int32)
     a[0], a[-1] = 0, k - 1
     check_logp(x, a, host(lrb.lr_policy_logp(dev(x), dev(a))))
+
+
+@pytest.mark.parametrize("k", (8192, 10007, 40007, 65536))
+@pytest.mark.parametrize("spread", (0.1, 2.0, 6.0))
+def test_clip_borders_of_long_rows(lrb, k, spread):
+    """Ratios within float32's error of a border, where a row's sum is longest: the side is the one that 64 bits say."""
+    g = rng(26, k)
+    r, s = 12, 24
+    low, high = 1.0 - float(np.float32(0.2)), 1.0 + float(np.float32(0.28))
+    x = (spread * g.standard_normal((r, k))).astype(np.float32)
+    a = g.integers(0, k, (s, r)).astype(np.int32)
+    lp = ot.policy_logp(x, a)
+    adv = np.where(g.uniform(size=(s, r)) < 0.5, 1.0, -1.0).astype(np.float32)
+    border = np.where(adv > 0, np.log(high), np.log(low))
+    away = g.uniform(-300 * U, 300 * U, (s, r))
+    old = (lp - border + away).astype(np.float32)
+    off = lp - old.astype(np.float64) - border
+    a[np.abs(off) < 1e-9] = -1
+    over = (a >= 0) & np.where(adv > 0, off > 0, off < 0)
+    kw = dict(clip_low=0.2, clip_high=0.28, kl_coef=0.0, entropy_coef=0.0, scale=1.0)
+    _, terms, grad, size, _ = ot.policy_loss(x, a, old, adv, **kw)
+    assert terms[3] == over.sum() and 0.3 < over.mean() < 0.7
+    _, got_terms, got = lrb.lr_policy_loss(dev(x), dev(a), dev(old), dev(adv), **kw)
+    assert float(got_terms[3]) == over.sum()
+    assert np.all(np.abs(host(got) - grad) <= parts_bound(x, s) * size + U * np.abs(grad) + 1e-40)
